@@ -405,6 +405,86 @@ eta_status_t eta_gated_prefill(const eta_prefill_desc_t* pd, const void* q, cons
                                void* out, float* R, float* L, void* stream);
 
 /*
+ * Norm and rotation of queries and keys, the step between the projections and
+ * attention: per head an RMS norm with a weight shared by the heads, then the
+ * rotation of the first rotary_dim values by the token's position, written in the
+ * layouts the other entry points read, q [batch][num_q_heads][new_tokens][head_dim]
+ * (new_tokens = 1: eta_decode's q; a prompt: eta_gated_prefill's) and the K / V caches.
+ *
+ * Token i of sequence b (i < new_tokens) is there when i < new_lens[b]; its position and
+ * its cache row are start[b] + i.  For a head's row x:
+ *   n = x / sqrt(mean(x^2) + eps) * weight          (n = x where the weight is NULL)
+ *   (a, b) -> (a cos f - b sin f, a sin f + b cos f),  f = position * freqs[j]
+ * for the pairs j < rotary_dim / 2: values j and j + rotary_dim / 2, or 2 j and 2 j + 1 when
+ * interleaved; values from rotary_dim on keep n.  v is copied to its cache.  Arithmetic in
+ * fp32 (angles reduced in fp64), rounded once.
+ *
+ * Tensors (dtype: ETA_DT_F32 or ETA_DT_BF16 for all of them; strides in elements, each row
+ * of head_dim contiguous, the heads of a token head_dim apart, every row 16-byte aligned):
+ *   q   element (b, i, h, c) at q[b*q_stride_b + i*q_stride_t + h*head_dim + c], h < num_q_heads
+ *   k, v  alike, h < num_kv_heads; the three may be parts of one fused projection's rows
+ *   caches  element (b, h, t, c) at k_cache[b*cache_stride_b + h*cache_stride_h + t*cache_stride_t + c],
+ *           t < capacity_tokens
+ * start and new_lens are device int32 [batch]; start NULL: 0 (negative values count as 0);
+ * new_lens NULL: new_tokens (values past new_tokens count as new_tokens).  q rows of tokens
+ * that are not there are left as they were, and so is every cache row but those of the tokens
+ * that are; a token whose cache row would be at or past capacity_tokens leaves none.
+ */
+typedef struct {
+  int32_t batch;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;        /* num_q_heads / num_kv_heads in {1, 2, 4, 8}; num_q_heads <= 256 */
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t new_tokens;          /* >= 1; batch * new_tokens < 2^31 - 64 */
+  int32_t dtype;               /* of q, k, v, the caches and their gradients */
+  int32_t rotary_dim;          /* a multiple of 16 in [0, head_dim]; 0: norm only */
+  int32_t interleaved;         /* 0 or 1 */
+  float eps;                   /* finite, >= 0 */
+  int32_t reserved;            /* 0 */
+  int64_t capacity_tokens;     /* rows per (sequence, kv head) of the caches, >= 1 */
+  int64_t q_stride_b, q_stride_t, k_stride_b, k_stride_t, v_stride_b, v_stride_t;
+  int64_t cache_stride_b, cache_stride_h, cache_stride_t;
+  int64_t dq_stride_b, dq_stride_t, dk_stride_b, dk_stride_t, dv_stride_b, dv_stride_t; /* backward */
+} eta_rope_desc_t;
+
+/*
+ * eta_qk_norm_rope -- the pass above.
+ *   v, v_cache   may both be NULL (queries and keys only)
+ *   q_weight, k_weight   fp32 [head_dim], or NULL
+ *   freqs        fp32 [rotary_dim / 2]; may be NULL when rotary_dim is 0
+ *   q_out        [batch][num_q_heads][new_tokens][head_dim], contiguous
+ * q_out and the caches must not overlap q, k and v.
+ */
+eta_status_t eta_qk_norm_rope(const eta_rope_desc_t* rd, const void* q, const void* k, const void* v,
+                              const float* q_weight, const float* k_weight, const float* freqs,
+                              const int32_t* start, const int32_t* new_lens, void* q_out,
+                              void* k_cache, void* v_cache, void* stream);
+
+/* Bytes of workspace eta_qk_norm_rope_backward needs (at least 256). */
+eta_status_t eta_qk_norm_rope_backward_workspace_size(const eta_rope_desc_t* rd, size_t* bytes);
+
+/*
+ * eta_qk_norm_rope_backward -- gradients of eta_qk_norm_rope: from those of its outputs to
+ * those of q, k, v and of the weights.
+ *   dq_out       [batch][num_q_heads][new_tokens][head_dim], contiguous
+ *   dk_cache, dv_cache   with the caches' strides: the gradients of cache rows start[b] + i
+ *   q, k         the forward's inputs (q may be NULL where q_weight is, k where k_weight is)
+ *   dq, dk, dv   with the strides dq_stride_b ..: gradients of q, k, v, in dtype; zero for tokens
+ *                that are not there (dk, dv: also where the cache had no row).  dv and dv_cache
+ *                may both be NULL
+ *   dq_weight, dk_weight   fp32 [head_dim], written (not added to); required where the weight
+ *                is given, ignored where it is NULL.  Sums in fp32 in a fixed order
+ *   workspace    >= eta_qk_norm_rope_backward_workspace_size() bytes, 256-byte aligned
+ */
+eta_status_t eta_qk_norm_rope_backward(const eta_rope_desc_t* rd, const void* dq_out,
+                                       const void* dk_cache, const void* dv_cache, const void* q,
+                                       const void* k, const float* q_weight, const float* k_weight,
+                                       const float* freqs, const int32_t* start,
+                                       const int32_t* new_lens, void* dq, void* dk, void* dv,
+                                       float* dq_weight, float* dk_weight, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
  * eta_block_bounds -- the screening bound of Eq. (dual_bound_eq) for every
  * full block and query head, as eta_decode computes it, without selecting or
  * attending.  For threshold calibration and diagnostics.
@@ -457,7 +537,14 @@ typedef enum {
   ETA_KERNEL_CALIB_ACCUMULATE = 8,
   ETA_KERNEL_CALIB_SOLVE = 9,
   ETA_KERNEL_PREFILL = 10,
-  ETA_KERNEL_KINDS = 11
+  ETA_KERNEL_KINDS = 11,        /* the kinds eta_profile_end writes */
+  ETA_KERNEL_QK_ROPE = 11,
+  ETA_KERNEL_QK_ROPE_GRAD = 12,
+  ETA_KERNEL_QK_WEIGHT_GRAD = 13,
+  ETA_KERNEL_PREFILL_GRAD_Q = 14,
+  ETA_KERNEL_PREFILL_GRAD_KV = 15,
+  ETA_KERNEL_PREFILL_GRAD_JOIN = 16,
+  ETA_KERNEL_ALL_KINDS = 17
 } eta_kernel_kind_t;
 
 typedef struct {
@@ -467,6 +554,9 @@ typedef struct {
 
 eta_status_t eta_profile_begin(void);
 eta_status_t eta_profile_end(eta_kernel_time_t* out /* [ETA_KERNEL_KINDS] */);
+/* The same for the first `kinds` kinds: out holds `kinds` entries (those past
+ * ETA_KERNEL_ALL_KINDS are written as zero). */
+eta_status_t eta_profile_end_all(eta_kernel_time_t* out, int32_t kinds);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libeta.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("eta_kernels.hip", "eta_prefill.hip", "eta_api.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("eta_kernels.hip", "eta_prefill.hip", "eta_api.cpp",
+                                           "eta_rope.hip", "eta_train_api.cpp")]
 # (source, extra flags, object name): eta_kernels.hip holds split decode on bf16
 # caches in part 1, on fp32 caches in part 2, and everything else in part 0
 UNITS = [(SOURCES[0], [f"-DETA_PART={p}"], f"eta_kernels.{p}.o") for p in (0, 1, 2)] + \
@@ -57,7 +58,7 @@ def _clean(stderr: str) -> str:
     return "\n".join(l for l in stderr.splitlines() if _NOISE not in l)
 
 
-def build(verbose: bool = False, jobs: int = 5) -> str:
+def build(verbose: bool = False, jobs: int = 8) -> str:
     """Compile every source to an object (in parallel), then link libeta.so."""
     objdir = tempfile.mkdtemp(prefix="eta_build_")
     try:

@@ -6,43 +6,13 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
-#include <cstring>
-#include <mutex>
-#include <string>
-#include <vector>
 
 #include "eta.h"
+#include "eta_host.h"
 #include "eta_internal.h"
 
 namespace eta {
 namespace {
-
-thread_local std::string g_err;
-
-eta_status_t fail(eta_status_t code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  std::vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  g_err = buf;
-  return code;
-}
-
-eta_status_t ok() {
-  g_err.clear();
-  return ETA_OK;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int elem_bytes(int dt) { return dt == ETA_DT_F32 ? 4 : 2; }
-
-bool valid_dtype(int dt) { return dt == ETA_DT_F32 || dt == ETA_DT_BF16; }
-
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Geometry checks shared by every entry point that takes an eta_kv_desc_t.
 eta_status_t check_kv(const eta_kv_desc_t* kv, Geom* g) {
@@ -137,49 +107,6 @@ eta_status_t check_params(const eta_decode_params_t* p) {
   if (p->num_splits < 0 || p->num_splits > kMaxSplits)
     return fail(ETA_ERR_INVALID_ARG, "num_splits must be in [0, %d]", kMaxSplits);
   return ETA_OK;
-}
-
-// ------------------------------------------------------------- kernel timer
-
-struct Profiler {
-  std::mutex mu;
-  bool on = false;
-  std::vector<hipEvent_t> pool;       // pairs: [2i] start, [2i+1] end
-  std::vector<int> kinds;
-  size_t used = 0;
-  static constexpr size_t kMaxPairs = 65536;
-};
-Profiler& prof() {
-  static Profiler p;
-  return p;
-}
-
-void hook_fn(int kind, hipStream_t st, bool after) {
-  Profiler& P = prof();
-  std::lock_guard<std::mutex> lk(P.mu);
-  if (!P.on) return;
-  if (!after) {
-    if (P.used >= Profiler::kMaxPairs) return;
-    if (2 * P.used + 2 > P.pool.size()) {
-      hipEvent_t a, b;
-      if (hipEventCreate(&a) != hipSuccess) return;
-      if (hipEventCreate(&b) != hipSuccess) { (void)hipEventDestroy(a); return; }
-      P.pool.push_back(a);
-      P.pool.push_back(b);
-    }
-    (void)hipEventRecord(P.pool[2 * P.used], st);
-    P.kinds.push_back(kind);
-  } else {
-    if (P.kinds.size() != P.used + 1) return;
-    (void)hipEventRecord(P.pool[2 * P.used + 1], st);
-    ++P.used;
-  }
-}
-
-LaunchHook active_hook() {
-  Profiler& P = prof();
-  std::lock_guard<std::mutex> lk(P.mu);
-  return P.on ? hook_fn : nullptr;
 }
 
 }  // namespace
@@ -686,11 +613,11 @@ eta_status_t eta_profile_begin(void) {
   return ok();
 }
 
-eta_status_t eta_profile_end(eta_kernel_time_t* out) {
+static eta_status_t profile_end_impl(eta_kernel_time_t* out, int kinds) {
   Profiler& P = prof();
   std::lock_guard<std::mutex> lk(P.mu);
   if (!out) return fail(ETA_ERR_INVALID_ARG, "out is NULL");
-  for (int i = 0; i < ETA_KERNEL_KINDS; ++i) out[i] = eta_kernel_time_t{0.0, 0};
+  for (int i = 0; i < kinds; ++i) out[i] = eta_kernel_time_t{0.0, 0};
   P.on = false;
   for (size_t i = 0; i < P.used; ++i) {
     hipError_t e = hipEventSynchronize(P.pool[2 * i + 1]);
@@ -699,7 +626,7 @@ eta_status_t eta_profile_end(eta_kernel_time_t* out) {
     e = hipEventElapsedTime(&ms, P.pool[2 * i], P.pool[2 * i + 1]);
     if (e != hipSuccess) return fail(ETA_ERR_HIP, "event elapsed time failed: %s", hipGetErrorString(e));
     const int k = P.kinds[i];
-    if (k >= 0 && k < ETA_KERNEL_KINDS) {
+    if (k >= 0 && k < kinds) {
       out[k].ms_total += ms;
       out[k].launches += 1;
     }
@@ -707,6 +634,13 @@ eta_status_t eta_profile_end(eta_kernel_time_t* out) {
   P.used = 0;
   P.kinds.clear();
   return ok();
+}
+
+eta_status_t eta_profile_end(eta_kernel_time_t* out) { return profile_end_impl(out, ETA_KERNEL_KINDS); }
+
+eta_status_t eta_profile_end_all(eta_kernel_time_t* out, int32_t kinds) {
+  if (kinds < 1) return fail(ETA_ERR_INVALID_ARG, "kinds must be >= 1 (got %d)", kinds);
+  return profile_end_impl(out, kinds);
 }
 
 }  // extern "C"

@@ -1,0 +1,184 @@
+// Host side of the operators around the gated prefill: argument validation, work
+// plans and the extern "C" entry points of the norm and rotation of queries and
+// keys and of its gradients.  As in eta_api.cpp every argument is checked before
+// anything is enqueued, and nothing is thrown across the ABI.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "eta.h"
+#include "eta_host.h"
+#include "eta_train.h"
+
+namespace eta {
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+eta_status_t check_heads(int hq, int hkv, int d) {
+  if (hq < 1 || hkv < 1 || hq % hkv != 0)
+    return fail(ETA_ERR_INVALID_ARG, "num_q_heads must be a positive multiple of num_kv_heads");
+  const int G = hq / hkv;
+  if (G != 1 && G != 2 && G != 4 && G != 8)
+    return fail(ETA_ERR_UNSUPPORTED, "GQA group size %d unsupported (1, 2, 4 or 8)", G);
+  if (hq > 256) return fail(ETA_ERR_UNSUPPORTED, "num_q_heads > 256 unsupported");
+  if (d != 64 && d != 128) return fail(ETA_ERR_UNSUPPORTED, "head_dim %d unsupported (64 or 128)", d);
+  return ETA_OK;
+}
+
+eta_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
+  if (!workspace) return fail(ETA_ERR_WORKSPACE, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+    return fail(ETA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (bytes < need) return fail(ETA_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", bytes, need);
+  return ETA_OK;
+}
+
+eta_status_t check_rope(const eta_rope_desc_t* rd) {
+  if (!rd) return fail(ETA_ERR_INVALID_ARG, "rotation descriptor is NULL");
+  if (rd->batch < 1 || rd->new_tokens < 1 || rd->capacity_tokens < 1)
+    return fail(ETA_ERR_INVALID_ARG, "batch, new_tokens and capacity_tokens must be >= 1");
+  if ((int64_t)rd->batch * rd->new_tokens >= (int64_t(1) << 31) - 64)
+    return fail(ETA_ERR_UNSUPPORTED, "batch * new_tokens must stay below 2^31 - 64");
+  if (eta_status_t st = check_heads(rd->num_q_heads, rd->num_kv_heads, rd->head_dim)) return st;
+  if (!valid_dtype(rd->dtype)) return fail(ETA_ERR_INVALID_ARG, "dtype %d is not ETA_DT_F32 or ETA_DT_BF16", rd->dtype);
+  if (rd->rotary_dim < 0 || rd->rotary_dim > rd->head_dim || rd->rotary_dim % 16 != 0)
+    return fail(ETA_ERR_INVALID_ARG, "rotary_dim %d must be a multiple of 16 in [0, head_dim]", rd->rotary_dim);
+  if (rd->interleaved != 0 && rd->interleaved != 1) return fail(ETA_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  if (rd->reserved != 0) return fail(ETA_ERR_INVALID_ARG, "reserved must be 0");
+  if (!std::isfinite(rd->eps) || rd->eps < 0.f) return fail(ETA_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  return ETA_OK;
+}
+
+// Strides of a projection [batch][new_tokens][heads][head_dim].  What is written may not
+// overlap itself: there neighbouring tokens and sequences must be a row of heads apart.
+eta_status_t check_rows(const eta_rope_desc_t& rd, const char* what, int heads, int64_t sb, int64_t st,
+                        bool written) {
+  const int64_t eb = elem_bytes(rd.dtype), row = (int64_t)heads * rd.head_dim;
+  if (sb < 0 || st < 0) return fail(ETA_ERR_INVALID_ARG, "%s: negative stride", what);
+  if ((sb * eb) % 16 || (st * eb) % 16)
+    return fail(ETA_ERR_INVALID_ARG, "%s: strides must keep rows 16-byte aligned", what);
+  if (written && ((rd.new_tokens > 1 && st < row) || (rd.batch > 1 && sb < row)))
+    return fail(ETA_ERR_INVALID_ARG, "%s: rows that are written overlap", what);
+  return ETA_OK;
+}
+
+eta_status_t check_cache(const eta_rope_desc_t& rd, bool written) {
+  const int64_t eb = elem_bytes(rd.dtype), d = rd.head_dim;
+  const int64_t sb = rd.cache_stride_b, sh = rd.cache_stride_h, st = rd.cache_stride_t;
+  if (sb < 0 || sh < 0 || st < 0) return fail(ETA_ERR_INVALID_ARG, "cache: negative stride");
+  if ((sb * eb) % 16 || (sh * eb) % 16 || (st * eb) % 16)
+    return fail(ETA_ERR_INVALID_ARG, "cache: strides must keep token rows 16-byte aligned");
+  if (st < d && rd.capacity_tokens > 1)
+    return fail(ETA_ERR_INVALID_ARG, "cache_stride_t (%lld) < head_dim (%d)", (long long)st, rd.head_dim);
+  if (written && ((rd.num_kv_heads > 1 && sh < d) || (rd.batch > 1 && sb < d)))
+    return fail(ETA_ERR_INVALID_ARG, "cache: rows that are written overlap");
+  return ETA_OK;
+}
+
+size_t rope_grad_bytes(const eta_rope_desc_t& rd, const RopePlan& p) {
+  return align256((size_t)(p.nq + p.nk) * p.steps * rd.head_dim * sizeof(float));
+}
+
+}  // namespace
+
+// A workgroup takes as many heads as still leave about four workgroups per compute unit
+// (sines and weights are formed once for them), at most 16.  Gradients: the workgroups along
+// the tiles are limited by the rows of partial weight gradients.
+RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad) {
+  RopePlan p{};
+  p.tile = 256 / (rd.head_dim * elem_bytes(rd.dtype) / 16);
+  p.tiles = (int)(((int64_t)rd.batch * rd.new_tokens + p.tile - 1) / p.tile);
+  for (p.heads = 16;; p.heads /= 2) {
+    p.nq = (rd.num_q_heads + p.heads - 1) / p.heads;
+    p.nk = (rd.num_kv_heads + p.heads - 1) / p.heads;
+    p.nv = has_v ? p.nk : 0;
+    if (p.heads == 1 || (int64_t)p.tiles * (p.nq + p.nk + p.nv) >= 1024) break;
+  }
+  const int most = kRopePartials / p.nq;      // nq >= nk, nq <= 256
+  p.steps = grad && p.tiles > most ? most : p.tiles;
+  return p;
+}
+
+}  // namespace eta
+
+using namespace eta;
+
+extern "C" {
+
+eta_status_t eta_qk_norm_rope(const eta_rope_desc_t* rd, const void* q, const void* k, const void* v,
+                              const float* q_weight, const float* k_weight, const float* freqs,
+                              const int32_t* start, const int32_t* new_lens, void* q_out,
+                              void* k_cache, void* v_cache, void* stream) {
+  if (eta_status_t st = check_rope(rd)) return st;
+  if (!q || !k || !q_out || !k_cache)
+    return fail(ETA_ERR_INVALID_ARG, "q, k, q_out and k_cache must be non-NULL");
+  if ((v == nullptr) != (v_cache == nullptr))
+    return fail(ETA_ERR_INVALID_ARG, "v and v_cache must be given together");
+  if (rd->rotary_dim > 0 && !freqs) return fail(ETA_ERR_INVALID_ARG, "freqs must be non-NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_cache) ||
+      !aligned16(v_cache))
+    return fail(ETA_ERR_INVALID_ARG, "q, k, v, q_out and the caches must be 16-byte aligned");
+  if (!aligned4(q_weight) || !aligned4(k_weight) || !aligned4(freqs) || !aligned4(start) || !aligned4(new_lens))
+    return fail(ETA_ERR_INVALID_ARG, "weights, freqs, start and new_lens must be 4-byte aligned");
+  if (eta_status_t st = check_rows(*rd, "q", rd->num_q_heads, rd->q_stride_b, rd->q_stride_t, false)) return st;
+  if (eta_status_t st = check_rows(*rd, "k", rd->num_kv_heads, rd->k_stride_b, rd->k_stride_t, false)) return st;
+  if (v)
+    if (eta_status_t st = check_rows(*rd, "v", rd->num_kv_heads, rd->v_stride_b, rd->v_stride_t, false)) return st;
+  if (eta_status_t st = check_cache(*rd, true)) return st;
+  hipError_t e = launch_rope(*rd, plan_rope(*rd, v != nullptr, false), q, k, v, q_weight, k_weight, freqs, start,
+                             new_lens, q_out, k_cache, v_cache, (hipStream_t)stream, active_hook());
+  if (e != hipSuccess) return fail(ETA_ERR_HIP, "rotation launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+eta_status_t eta_qk_norm_rope_backward_workspace_size(const eta_rope_desc_t* rd, size_t* bytes) {
+  if (eta_status_t st = check_rope(rd)) return st;
+  if (!bytes) return fail(ETA_ERR_INVALID_ARG, "bytes is NULL");
+  // (with and without v alike: the larger of the two plans)
+  const size_t a = rope_grad_bytes(*rd, plan_rope(*rd, true, true)), b = rope_grad_bytes(*rd, plan_rope(*rd, false, true));
+  *bytes = a > b ? a : b;
+  return ok();
+}
+
+eta_status_t eta_qk_norm_rope_backward(const eta_rope_desc_t* rd, const void* dq_out,
+                                       const void* dk_cache, const void* dv_cache, const void* q,
+                                       const void* k, const float* q_weight, const float* k_weight,
+                                       const float* freqs, const int32_t* start,
+                                       const int32_t* new_lens, void* dq, void* dk, void* dv,
+                                       float* dq_weight, float* dk_weight, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  if (eta_status_t st = check_rope(rd)) return st;
+  if (!dq_out || !dk_cache || !dq || !dk)
+    return fail(ETA_ERR_INVALID_ARG, "dq_out, dk_cache, dq and dk must be non-NULL");
+  if ((dv == nullptr) != (dv_cache == nullptr))
+    return fail(ETA_ERR_INVALID_ARG, "dv and dv_cache must be given together");
+  if (rd->rotary_dim > 0 && !freqs) return fail(ETA_ERR_INVALID_ARG, "freqs must be non-NULL");
+  if ((q_weight && (!q || !dq_weight)) || (k_weight && (!k || !dk_weight)))
+    return fail(ETA_ERR_INVALID_ARG, "a weight needs the forward's input and its gradient's buffer");
+  if (!aligned16(dq_out) || !aligned16(dk_cache) || !aligned16(dv_cache) || !aligned16(q) || !aligned16(k) ||
+      !aligned16(dq) || !aligned16(dk) || !aligned16(dv))
+    return fail(ETA_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+  if (!aligned4(q_weight) || !aligned4(k_weight) || !aligned4(freqs) || !aligned4(start) || !aligned4(new_lens) ||
+      !aligned4(dq_weight) || !aligned4(dk_weight))
+    return fail(ETA_ERR_INVALID_ARG, "weights, their gradients, freqs, start and new_lens must be 4-byte aligned");
+  if (q_weight)
+    if (eta_status_t st = check_rows(*rd, "q", rd->num_q_heads, rd->q_stride_b, rd->q_stride_t, false)) return st;
+  if (k_weight)
+    if (eta_status_t st = check_rows(*rd, "k", rd->num_kv_heads, rd->k_stride_b, rd->k_stride_t, false)) return st;
+  if (eta_status_t st = check_rows(*rd, "dq", rd->num_q_heads, rd->dq_stride_b, rd->dq_stride_t, true)) return st;
+  if (eta_status_t st = check_rows(*rd, "dk", rd->num_kv_heads, rd->dk_stride_b, rd->dk_stride_t, true)) return st;
+  if (dv)
+    if (eta_status_t st = check_rows(*rd, "dv", rd->num_kv_heads, rd->dv_stride_b, rd->dv_stride_t, true)) return st;
+  if (eta_status_t st = check_cache(*rd, false)) return st;
+  const RopePlan p = plan_rope(*rd, dv != nullptr, true);
+  if (eta_status_t st = check_workspace(workspace, workspace_bytes, rope_grad_bytes(*rd, p))) return st;
+  hipError_t e = launch_rope_grad(*rd, p, dq_out, dk_cache, dv_cache, q, k, q_weight, k_weight, freqs, start,
+                                  new_lens, dq, dk, dv, dq_weight, dk_weight, (float*)workspace,
+                                  (hipStream_t)stream, active_hook());
+  if (e != hipSuccess) return fail(ETA_ERR_HIP, "rotation gradient launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+}  // extern "C"

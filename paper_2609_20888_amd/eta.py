@@ -20,7 +20,9 @@ LIB_PATH = os.path.join(_HERE, "libeta.so")
 ETA_OK, ETA_ERR_INVALID_ARG, ETA_ERR_UNSUPPORTED, ETA_ERR_WORKSPACE, ETA_ERR_HIP = range(5)
 ETA_DT_F32, ETA_DT_BF16, ETA_DT_F16, ETA_DT_FP8 = 0, 1, 2, 3
 KERNEL_KINDS = ("summaries", "predict", "screen", "split_decode", "combine", "dense_split",
-                "dense_combine", "bounds", "calib_accumulate", "calib_solve", "prefill")
+                "dense_combine", "bounds", "calib_accumulate", "calib_solve", "prefill",
+                "qk_rope", "qk_rope_grad", "qk_weight_grad", "prefill_grad_q", "prefill_grad_kv",
+                "prefill_grad_join")
 
 _vp = ctypes.c_void_p
 
@@ -57,6 +59,18 @@ class PrefillDesc(ctypes.Structure):
                 ("beta", ctypes.c_float), ("additive", ctypes.c_int32), ("C", ctypes.c_float)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "num_q_heads", "num_kv_heads", "head_dim",
+                                              "new_tokens", "dtype", "rotary_dim", "interleaved")] + \
+               [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("capacity_tokens",
+                                              "q_stride_b", "q_stride_t", "k_stride_b", "k_stride_t",
+                                              "v_stride_b", "v_stride_t", "cache_stride_b",
+                                              "cache_stride_h", "cache_stride_t",
+                                              "dq_stride_b", "dq_stride_t", "dk_stride_b",
+                                              "dk_stride_t", "dv_stride_b", "dv_stride_t")]
+
+
 class DecodeParams(ctypes.Structure):
     _fields_ = [("beta", ctypes.c_float), ("z", ctypes.c_float), ("offset_a", ctypes.c_float),
                 ("rescue_window_blocks", ctypes.c_int32), ("pin_recent_blocks", ctypes.c_int32),
@@ -73,6 +87,8 @@ EXPORTS = ("eta_build_block_summaries", "eta_build_block_summaries_envelope",
            "eta_update_block_summaries", "eta_predict_threshold", "eta_decode_workspace_size",
            "eta_decode", "eta_decode_predicted", "eta_decode_predicted_noalloc", "eta_block_bounds", "eta_dense_workspace_size", "eta_dense_decode",
            "eta_calib_accumulate", "eta_calib_solve", "eta_gated_prefill",
+           "eta_qk_norm_rope", "eta_qk_norm_rope_backward_workspace_size",
+           "eta_qk_norm_rope_backward", "eta_profile_end_all",
            "eta_last_error_string", "eta_abi_version", "eta_profile_begin", "eta_profile_end")
 
 
@@ -116,6 +132,10 @@ def load_library(path: Optional[str] = None):
         "eta_block_bounds": [P(KvDesc), i32, _vp, _vp, P(SummaryDesc), f32, _vp, _vp],
         "eta_dense_workspace_size": [P(KvDesc), i32, P(sz)],
         "eta_dense_decode": [P(KvDesc), i32, _vp, _vp, _vp, _vp, _vp, i32, _vp, sz, _vp],
+        "eta_qk_norm_rope": [P(RopeDesc)] + [_vp] * 12,
+        "eta_qk_norm_rope_backward_workspace_size": [P(RopeDesc), P(sz)],
+        "eta_qk_norm_rope_backward": [P(RopeDesc)] + [_vp] * 16 + [sz, _vp],
+        "eta_profile_end_all": [P(KernelTime), i32],
         "eta_profile_begin": [],
         "eta_profile_end": [P(KernelTime)],
     }
@@ -463,7 +483,7 @@ def profile_begin():
 
 def profile_end() -> dict:
     arr = (KernelTime * len(KERNEL_KINDS))()
-    _check(load_library().eta_profile_end(arr))
+    _check(load_library().eta_profile_end_all(arr, len(KERNEL_KINDS)))
     return {name: (arr[i].ms_total, arr[i].launches) for i, name in enumerate(KERNEL_KINDS)}
 
 
@@ -536,3 +556,207 @@ def gated_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: torch.
                                             _ptr(tau), _ptr(seq_lens), _ptr(out), _ptr(R), _ptr(L),
                                             _stream(stream)))
     return out, R, L
+
+
+# ---------------------------------------------------------------- around the prefill
+
+def _on_one_gpu(q: torch.Tensor, *others) -> torch.device:
+    """The GPU that holds q; raises unless every tensor given is there."""
+    if q.device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {q.device}")
+    for t in others:
+        if t is not None and t.device != q.device:
+            raise ValueError(f"tensors must be on one device, got {q.device} and {t.device}")
+    return q.device
+
+
+class _On:
+    """Makes a device current for a call and gives the stream the call is for."""
+
+    def __init__(self, device: torch.device, stream=None):
+        s = stream if stream is not None else torch.cuda.current_stream(device)
+        if s.device != device:
+            raise ValueError(f"the stream is on {s.device}, the tensors on {device}")
+        self.stream = _vp(s.cuda_stream)
+        self.index = device.index
+        self.before = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.index:
+            self.before = torch.cuda.current_device()
+            torch.cuda.set_device(self.index)
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
+
+
+def _vector(name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> None:
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be {dtype} [{n}] contiguous, got {t.dtype} {tuple(t.shape)}")
+
+
+def _heads_apart(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
+    """[B][T][H][d] with the heads of a token d apart (a part of a fused projection's rows is)."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.stride(3) != 1 or (shape[2] > 1 and t.stride(2) != shape[3]):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+
+
+def _step(t: torch.Tensor, dim: int) -> int:
+    """The stride of a dimension; of one of size one, whose stride means nothing, zero."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _plain(name: str, t: torch.Tensor, shape, dtype: torch.dtype) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} contiguous, got {t.dtype} {tuple(t.shape)}")
+
+
+def _rope_desc(B, Hq, Hkv, d, T, dtype, freqs, q_weight, k_weight, eps, interleaved, start, new_lens,
+               k_cache, v_cache) -> RopeDesc:
+    """The descriptor without the projections' strides, and the checks the C call cannot make."""
+    if freqs is not None:
+        _vector("freqs", freqs, freqs.numel(), torch.float32)
+    _vector("q_weight", q_weight, d, torch.float32)
+    _vector("k_weight", k_weight, d, torch.float32)
+    _vector("start", start, B, torch.int32)
+    _vector("new_lens", new_lens, B, torch.int32)
+    if k_cache.dim() != 4 or k_cache.stride(3) != 1 or k_cache.dtype != dtype or \
+            (k_cache.shape[0], k_cache.shape[1], k_cache.shape[3]) != (B, Hkv, d):
+        raise ValueError(f"the K cache must be {dtype} [{B}][{Hkv}][T_cap][{d}], the head dimension "
+                         f"contiguous, got {k_cache.dtype} {tuple(k_cache.shape)}")
+    if v_cache is not None and (v_cache.shape != k_cache.shape or v_cache.dtype != dtype
+                                or any(_step(v_cache, i) != _step(k_cache, i) for i in range(3))
+                                or v_cache.stride(3) != 1):
+        raise ValueError("the K and V caches must share shape, strides and dtype")
+    return RopeDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, new_tokens=T,
+                    dtype=ETA_DT_F32 if dtype == torch.float32 else ETA_DT_BF16,
+                    rotary_dim=0 if freqs is None else 2 * freqs.numel(),
+                    interleaved=int(bool(interleaved)), eps=eps, capacity_tokens=k_cache.shape[2],
+                    cache_stride_b=_step(k_cache, 0), cache_stride_h=_step(k_cache, 1),
+                    cache_stride_t=_step(k_cache, 2))
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = None, *,
+                 freqs: Optional[torch.Tensor], q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 interleaved: bool = False, start: Optional[torch.Tensor] = None,
+                 new_lens: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
+                 stream=None):
+    """eta_qk_norm_rope: RMS norm and rotation of each head of q and k, into q [B][Hq][T][d]
+    and the caches (v is copied).  q [B][T][Hq][d], k, v [B][T][Hkv][d] (float32 or bfloat16;
+    views of a fused projection do), freqs fp32 [rotary_dim / 2] or None, weights fp32 [d] or
+    None (no norm), start / new_lens int32 [B].  Token i of sequence b is at position and cache
+    row start[b] + i; rows of tokens from new_lens[b] on are left as they were.  Caches that are
+    not given are allocated with T rows (start must then be None).  Returns (q, k_cache,
+    v_cache); for a single token q is what a decode step reads, viewed as [B][Hq][d]."""
+    B, T, Hq, d = q.shape
+    Hkv = k.shape[2]
+    dt = q.dtype
+    _dtype_code(q)
+    dev = _on_one_gpu(q, k, v, freqs, q_weight, k_weight, start, new_lens, q_out, k_cache, v_cache)
+    _heads_apart("q", q, (B, T, Hq, d), dt)
+    _heads_apart("k", k, (B, T, Hkv, d), dt)
+    _heads_apart("v", v, (B, T, Hkv, d), dt)
+    if k_cache is None or (v is not None and v_cache is None):
+        if start is not None or k_cache is not None or v_cache is not None:
+            raise ValueError("start and a cache come with both caches")
+        k_cache = torch.empty(B, Hkv, T, d, device=dev, dtype=dt)
+        v_cache = None if v is None else torch.empty_like(k_cache)
+    if q_out is None:
+        q_out = torch.empty(B, Hq, T, d, device=dev, dtype=dt)
+    _plain("q_out", q_out, (B, Hq, T, d), dt)
+    rd = _rope_desc(B, Hq, Hkv, d, T, dt, freqs, q_weight, k_weight, eps, interleaved, start, new_lens,
+                    k_cache, v_cache if v is not None else None)
+    rd.q_stride_b, rd.q_stride_t = _step(q, 0), _step(q, 1)
+    rd.k_stride_b, rd.k_stride_t = _step(k, 0), _step(k, 1)
+    if v is not None:
+        rd.v_stride_b, rd.v_stride_t = _step(v, 0), _step(v, 1)
+    with _On(dev, stream) as s:
+        _check(load_library().eta_qk_norm_rope(
+            ctypes.byref(rd), _ptr(q), _ptr(k), _ptr(v), _ptr(q_weight), _ptr(k_weight), _ptr(freqs),
+            _ptr(start), _ptr(new_lens), _ptr(q_out), _ptr(k_cache),
+            _ptr(v_cache) if v is not None else None, s))
+    return q_out, k_cache, v_cache
+
+
+def qk_norm_rope_backward(dq_out: torch.Tensor, dk_cache: torch.Tensor,
+                          dv_cache: Optional[torch.Tensor], q: torch.Tensor, k: torch.Tensor, *,
+                          freqs: Optional[torch.Tensor], q_weight: Optional[torch.Tensor] = None,
+                          k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                          interleaved: bool = False, start: Optional[torch.Tensor] = None,
+                          new_lens: Optional[torch.Tensor] = None,
+                          dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                          dv: Optional[torch.Tensor] = None,
+                          dq_weight: Optional[torch.Tensor] = None,
+                          dk_weight: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None):
+    """eta_qk_norm_rope_backward: from the gradients of qk_norm_rope's outputs (dq_out
+    [B][Hq][T][d], dk_cache and dv_cache in the caches' shape, rows start[b] + i) and its inputs
+    q, k to (dq, dk, dv, dq_weight, dk_weight).  dq, dk, dv [B][T][H][d] (given: may be views of a
+    fused gradient), zero for tokens from new_lens[b] on; the weights' gradients fp32 [d], None
+    where the weight is; dv None where dv_cache is."""
+    B, T, Hq, d = q.shape
+    Hkv = k.shape[2]
+    dt = q.dtype
+    _dtype_code(q)
+    dev = _on_one_gpu(q, k, dq_out, dk_cache, dv_cache, freqs, q_weight, k_weight, start, new_lens, dq, dk, dv,
+                      dq_weight, dk_weight, workspace)
+    _heads_apart("q", q, (B, T, Hq, d), dt)
+    _heads_apart("k", k, (B, T, Hkv, d), dt)
+    _plain("dq_out", dq_out, (B, Hq, T, d), dt)
+    rd = _rope_desc(B, Hq, Hkv, d, T, dt, freqs, q_weight, k_weight, eps, interleaved, start, new_lens,
+                    dk_cache, dv_cache)
+    if dq is None:
+        dq = torch.empty(B, T, Hq, d, device=dev, dtype=dt)
+    if dk is None:
+        dk = torch.empty(B, T, Hkv, d, device=dev, dtype=dt)
+    if dv_cache is None:
+        dv = None
+    elif dv is None:
+        dv = torch.empty(B, T, Hkv, d, device=dev, dtype=dt)
+    _heads_apart("dq", dq, (B, T, Hq, d), dt)
+    _heads_apart("dk", dk, (B, T, Hkv, d), dt)
+    _heads_apart("dv", dv, (B, T, Hkv, d), dt)
+    if q_weight is None:
+        dq_weight = None
+    elif dq_weight is None:
+        dq_weight = torch.empty_like(q_weight)
+    if k_weight is None:
+        dk_weight = None
+    elif dk_weight is None:
+        dk_weight = torch.empty_like(k_weight)
+    _vector("dq_weight", dq_weight, d, torch.float32)
+    _vector("dk_weight", dk_weight, d, torch.float32)
+    rd.q_stride_b, rd.q_stride_t = _step(q, 0), _step(q, 1)
+    rd.k_stride_b, rd.k_stride_t = _step(k, 0), _step(k, 1)
+    rd.dq_stride_b, rd.dq_stride_t = _step(dq, 0), _step(dq, 1)
+    rd.dk_stride_b, rd.dk_stride_t = _step(dk, 0), _step(dk, 1)
+    if dv is not None:
+        rd.dv_stride_b, rd.dv_stride_t = _step(dv, 0), _step(dv, 1)
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check(lib.eta_qk_norm_rope_backward_workspace_size(ctypes.byref(rd), ctypes.byref(n)))
+    workspace = _workspace(workspace, n.value, dev)
+    with _On(dev, stream) as s:
+        _check(lib.eta_qk_norm_rope_backward(
+            ctypes.byref(rd), _ptr(dq_out), _ptr(dk_cache), _ptr(dv_cache), _ptr(q), _ptr(k),
+            _ptr(q_weight), _ptr(k_weight), _ptr(freqs), _ptr(start), _ptr(new_lens), _ptr(dq),
+            _ptr(dk), _ptr(dv), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), s))
+    return dq, dk, dv, dq_weight, dk_weight
+
+
+def _workspace(given: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
+    """The caller's workspace where it is large enough, else a new one."""
+    if given is not None and not given.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    if given is None or given.numel() * given.element_size() < nbytes:
+        return alloc_workspace(nbytes, device)
+    return given
