@@ -405,6 +405,36 @@ eta_status_t eta_gated_prefill(const eta_prefill_desc_t* pd, const void* q, cons
                                void* out, float* R, float* L, void* stream);
 
 /*
+ * eta_gated_prefill_backward -- gradients of eta_gated_prefill (Alg. bwd_kernel):
+ * from those of out, R and L to those of q, k, v and tau.  The probabilities
+ * P = exp(S~ - L) are formed again; with D_i = <dout_i, out_i> - dL_i,
+ *   dS~_ij = P_ij (<dout_i, v_j> - D_i),  m_ij = beta (S_ij dS~_ij + dR_i)
+ *            (additive: beta (C dS~_ij + dR_i); on the diagonal beta dR_i),
+ *   dS_ij  = dS~_ij sigma_ij + sigma_ij (1 - sigma_ij) m_ij
+ *            (additive and on the diagonal: dS~_ij + sigma_ij (1 - sigma_ij) m_ij),
+ *   dtau_i = - sum_j sigma_ij (1 - sigma_ij) m_ij,  dv_j = sum_i P_ij dout_i,
+ *   dq_i   = sum_j dS_ij k_j / sqrt(head_dim),  dk_j = sum_i dS_ij q_i / sqrt(head_dim),
+ * dk and dv over every query head of the kv head's group.  Products on the matrix cores
+ * (bf16 operands, fp32 accumulation; P and dS are rounded to bf16 for theirs), everything
+ * else fp32; sums in a fixed order (bitwise reproducible).
+ *   pd          as for the forward; capacity_tokens <= 2^24
+ *   q, k, v, tau, seq_lens   the forward's inputs
+ *   out, L      the forward's results for them
+ *   dout        bf16, like out;  dR, dL  fp32, like R and L, or NULL (zero)
+ *   dq, dk, dv  bf16, like q, k, v;  dtau  fp32, like tau.  Rows from seq_lens[b] on: zero;
+ *               nothing that the inputs hold there reaches a result.  No output may overlap
+ *               an input or another output
+ *   workspace   >= eta_gated_prefill_backward_workspace_size() bytes, 256-byte aligned
+ */
+eta_status_t eta_gated_prefill_backward_workspace_size(const eta_prefill_desc_t* pd, size_t* bytes);
+eta_status_t eta_gated_prefill_backward(const eta_prefill_desc_t* pd, const void* q, const void* k,
+                                        const void* v, const float* tau, const int32_t* seq_lens,
+                                        const void* out, const float* L, const void* dout,
+                                        const float* dR, const float* dL, void* dq, void* dk,
+                                        void* dv, float* dtau, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/*
  * Norm and rotation of queries and keys, the step between the projections and
  * attention: per head an RMS norm with a weight shared by the heads, then the
  * rotation of the first rotary_dim values by the token's position, written in the

@@ -21,7 +21,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libeta.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("eta_kernels.hip", "eta_prefill.hip", "eta_api.cpp",
-                                           "eta_rope.hip", "eta_train_api.cpp")]
+                                           "eta_prefill_grad.hip", "eta_rope.hip",
+                                           "eta_train_api.cpp")]
 # (source, extra flags, object name): eta_kernels.hip holds split decode on bf16
 # caches in part 1, on fp32 caches in part 2, and everything else in part 0
 UNITS = [(SOURCES[0], [f"-DETA_PART={p}"], f"eta_kernels.{p}.o") for p in (0, 1, 2)] + \
@@ -39,7 +40,7 @@ def hipcc() -> str:
 # MFMA results kept in the ordinary vector registers: for the prefill kernel only
 # (no copies between accumulation and arithmetic registers there; the
 # calibration kernel is faster with the default register classes)
-VGPR_FORM = {"eta_prefill.hip"}
+VGPR_FORM = {"eta_prefill.hip", "eta_prefill_grad.hip"}
 
 
 def _flags(src: str):

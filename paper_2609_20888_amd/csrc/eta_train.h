@@ -37,4 +37,28 @@ hipError_t launch_rope_grad(const eta_rope_desc_t& rd, const RopePlan& p, const 
                             void* dv, float* dqw, float* dkw, float* part, hipStream_t stream,
                             LaunchHook hook);
 
+// Work of a call of the prefill's gradients: blocks of 128 rows per (head, sequence), the
+// rows of a head's scalars in the workspace (whole blocks), and the parts that the heads of a
+// kv group are split into (partial dk, dv in the workspace when there are several).
+struct GradPlan {
+  int blocks;
+  int rows;
+  int nsplit;
+};
+GradPlan plan_prefill_grad(const eta_prefill_desc_t& pd);
+
+struct PrefillGradPtrs {
+  const void *q, *k, *v, *out, *dout;
+  const float *tau, *L, *dR, *dL;
+  const int32_t* seq_lens;
+  void *dq, *dk, *dv;
+  float* dtau;
+  float* stats;              // [4][batch num_q_heads][rows]
+  float* part;               // [2][nsplit][batch num_kv_heads][capacity_tokens][head_dim], nsplit > 1
+};
+size_t prefill_grad_bytes(const eta_prefill_desc_t& pd, const GradPlan& p, PrefillGradPtrs* carve, void* base);
+
+hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, const PrefillGradPtrs& x,
+                               hipStream_t stream, LaunchHook hook);
+
 }  // namespace eta

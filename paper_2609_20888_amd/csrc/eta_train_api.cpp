@@ -1,6 +1,6 @@
 // Host side of the operators around the gated prefill: argument validation, work
 // plans and the extern "C" entry points of the norm and rotation of queries and
-// keys and of its gradients.  As in eta_api.cpp every argument is checked before
+// keys, of its gradients and of the prefill's gradients.  As in eta_api.cpp every argument is checked before
 // anything is enqueued, and nothing is thrown across the ABI.
 
 #include <hip/hip_runtime.h>
@@ -77,6 +77,20 @@ eta_status_t check_cache(const eta_rope_desc_t& rd, bool written) {
   return ETA_OK;
 }
 
+eta_status_t check_prefill(const eta_prefill_desc_t* pd) {
+  if (!pd) return fail(ETA_ERR_INVALID_ARG, "prefill descriptor is NULL");
+  if (pd->batch < 1 || pd->batch > 65535 || pd->capacity_tokens < 1)
+    return fail(ETA_ERR_INVALID_ARG, "batch must be in [1, 65535] and capacity_tokens >= 1");
+  if (pd->capacity_tokens > (1 << 24)) return fail(ETA_ERR_UNSUPPORTED, "capacity_tokens > 2^24 unsupported");
+  if (eta_status_t st = check_heads(pd->num_q_heads, pd->num_kv_heads, pd->head_dim)) return st;
+  if (pd->dtype != ETA_DT_BF16) return fail(ETA_ERR_UNSUPPORTED, "the prefill's gradients take bf16 q, k, v");
+  if (!std::isfinite(pd->beta) || pd->beta < 0.f)
+    return fail(ETA_ERR_INVALID_ARG, "beta must be finite and >= 0");
+  if (pd->additive != 0 && pd->additive != 1) return fail(ETA_ERR_INVALID_ARG, "additive must be 0 or 1");
+  if (pd->additive && !std::isfinite(pd->C)) return fail(ETA_ERR_INVALID_ARG, "C must be finite");
+  return ETA_OK;
+}
+
 size_t rope_grad_bytes(const eta_rope_desc_t& rd, const RopePlan& p) {
   return align256((size_t)(p.nq + p.nk) * p.steps * rd.head_dim * sizeof(float));
 }
@@ -99,6 +113,30 @@ RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad) {
   const int most = kRopePartials / p.nq;      // nq >= nk, nq <= 256
   p.steps = grad && p.tiles > most ? most : p.tiles;
   return p;
+}
+
+GradPlan plan_prefill_grad(const eta_prefill_desc_t& pd) {
+  GradPlan p;
+  p.blocks = (pd.capacity_tokens + 127) / 128;
+  p.rows = 128 * p.blocks;
+  p.nsplit = 1;
+  const int64_t wgs = (int64_t)p.blocks * pd.num_kv_heads * pd.batch;
+  const int G = pd.num_q_heads / pd.num_kv_heads;
+  while (p.nsplit < G && wgs * p.nsplit < 512) p.nsplit *= 2;
+  return p;
+}
+
+size_t prefill_grad_bytes(const eta_prefill_desc_t& pd, const GradPlan& p, PrefillGradPtrs* c, void* base) {
+  const size_t o_part = align256((size_t)4 * pd.batch * pd.num_q_heads * p.rows * sizeof(float));
+  size_t off = o_part;
+  if (p.nsplit > 1)
+    off = align256(off + (size_t)2 * p.nsplit * pd.batch * pd.num_kv_heads * pd.capacity_tokens * pd.head_dim *
+                             sizeof(float));
+  if (c && base) {
+    c->stats = static_cast<float*>(base);
+    c->part = p.nsplit > 1 ? reinterpret_cast<float*>(static_cast<char*>(base) + o_part) : nullptr;
+  }
+  return off;
 }
 
 }  // namespace eta
@@ -178,6 +216,37 @@ eta_status_t eta_qk_norm_rope_backward(const eta_rope_desc_t* rd, const void* dq
                                   new_lens, dq, dk, dv, dq_weight, dk_weight, (float*)workspace,
                                   (hipStream_t)stream, active_hook());
   if (e != hipSuccess) return fail(ETA_ERR_HIP, "rotation gradient launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+eta_status_t eta_gated_prefill_backward_workspace_size(const eta_prefill_desc_t* pd, size_t* bytes) {
+  if (eta_status_t st = check_prefill(pd)) return st;
+  if (!bytes) return fail(ETA_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = prefill_grad_bytes(*pd, plan_prefill_grad(*pd), nullptr, nullptr);
+  return ok();
+}
+
+eta_status_t eta_gated_prefill_backward(const eta_prefill_desc_t* pd, const void* q, const void* k,
+                                        const void* v, const float* tau, const int32_t* seq_lens,
+                                        const void* out, const float* L, const void* dout,
+                                        const float* dR, const float* dL, void* dq, void* dk, void* dv,
+                                        float* dtau, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+  if (eta_status_t st = check_prefill(pd)) return st;
+  if (!q || !k || !v || !tau || !seq_lens || !out || !L || !dout)
+    return fail(ETA_ERR_INVALID_ARG, "q, k, v, tau, seq_lens, out, L and dout must be non-NULL");
+  if (!dq || !dk || !dv || !dtau) return fail(ETA_ERR_INVALID_ARG, "dq, dk, dv and dtau must be non-NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(dout) || !aligned16(dq) ||
+      !aligned16(dk) || !aligned16(dv))
+    return fail(ETA_ERR_INVALID_ARG, "q, k, v, out and their gradients must be 16-byte aligned");
+  if (!aligned4(tau) || !aligned4(L) || !aligned4(dR) || !aligned4(dL) || !aligned4(seq_lens) || !aligned4(dtau))
+    return fail(ETA_ERR_INVALID_ARG, "tau, L, dR, dL, seq_lens and dtau must be 4-byte aligned");
+  const GradPlan p = plan_prefill_grad(*pd);
+  PrefillGradPtrs x{q, k, v, out, dout, tau, L, dR, dL, seq_lens, dq, dk, dv, dtau, nullptr, nullptr};
+  if (eta_status_t st = check_workspace(workspace, workspace_bytes, prefill_grad_bytes(*pd, p, &x, workspace)))
+    return st;
+  hipError_t e = launch_prefill_grad(*pd, p, x, (hipStream_t)stream, active_hook());
+  if (e != hipSuccess) return fail(ETA_ERR_HIP, "prefill gradient launch failed: %s", hipGetErrorString(e));
   return ok();
 }
 

@@ -87,6 +87,7 @@ EXPORTS = ("eta_build_block_summaries", "eta_build_block_summaries_envelope",
            "eta_update_block_summaries", "eta_predict_threshold", "eta_decode_workspace_size",
            "eta_decode", "eta_decode_predicted", "eta_decode_predicted_noalloc", "eta_block_bounds", "eta_dense_workspace_size", "eta_dense_decode",
            "eta_calib_accumulate", "eta_calib_solve", "eta_gated_prefill",
+           "eta_gated_prefill_backward_workspace_size", "eta_gated_prefill_backward",
            "eta_qk_norm_rope", "eta_qk_norm_rope_backward_workspace_size",
            "eta_qk_norm_rope_backward", "eta_profile_end_all",
            "eta_last_error_string", "eta_abi_version", "eta_profile_begin", "eta_profile_end")
@@ -132,6 +133,8 @@ def load_library(path: Optional[str] = None):
         "eta_block_bounds": [P(KvDesc), i32, _vp, _vp, P(SummaryDesc), f32, _vp, _vp],
         "eta_dense_workspace_size": [P(KvDesc), i32, P(sz)],
         "eta_dense_decode": [P(KvDesc), i32, _vp, _vp, _vp, _vp, _vp, i32, _vp, sz, _vp],
+        "eta_gated_prefill_backward_workspace_size": [P(PrefillDesc), P(sz)],
+        "eta_gated_prefill_backward": [P(PrefillDesc)] + [_vp] * 15 + [sz, _vp],
         "eta_qk_norm_rope": [P(RopeDesc)] + [_vp] * 12,
         "eta_qk_norm_rope_backward_workspace_size": [P(RopeDesc), P(sz)],
         "eta_qk_norm_rope_backward": [P(RopeDesc)] + [_vp] * 16 + [sz, _vp],
@@ -760,3 +763,49 @@ def _workspace(given: Optional[torch.Tensor], nbytes: int, device) -> torch.Tens
     if given is None or given.numel() * given.element_size() < nbytes:
         return alloc_workspace(nbytes, device)
     return given
+
+
+def gated_prefill_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: torch.Tensor,
+                           seq_lens: torch.Tensor, out: torch.Tensor, L: torch.Tensor,
+                           dout: torch.Tensor, *, dR: Optional[torch.Tensor] = None,
+                           dL: Optional[torch.Tensor] = None, beta: float, additive: bool = False,
+                           C: float = 0.0, dq: Optional[torch.Tensor] = None,
+                           dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                           dtau: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """eta_gated_prefill_backward: gradients of gated_prefill.  q, k, v, tau, seq_lens, beta,
+    additive and C as given to it, out and L as it returned them, dout bf16 [B][Hq][T][d] the
+    output's gradient, dR and dL fp32 [B][Hq][T] those of the gate row sums and the log-sum-exp
+    (None: zero); returns (dq, dk, dv bf16, dtau fp32), zero past each sequence's end."""
+    B, Hq, T, d = q.shape
+    Hkv = k.shape[1]
+    bf, f32 = torch.bfloat16, torch.float32
+    dev = _on_one_gpu(q, k, v, tau, seq_lens, out, L, dout, dR, dL, dq, dk, dv, dtau, workspace)
+    qs, ks, rs = (B, Hq, T, d), (B, Hkv, T, d), (B, Hq, T)
+    if dq is None:
+        dq = torch.empty(qs, device=dev, dtype=bf)
+    if dk is None:
+        dk = torch.empty(ks, device=dev, dtype=bf)
+    if dv is None:
+        dv = torch.empty(ks, device=dev, dtype=bf)
+    if dtau is None:
+        dtau = torch.empty(rs, device=dev, dtype=f32)
+    for name, t, shape, dt in (("q", q, qs, bf), ("k", k, ks, bf), ("v", v, ks, bf), ("tau", tau, rs, f32),
+                               ("out", out, qs, bf), ("L", L, rs, f32), ("dout", dout, qs, bf),
+                               ("dR", dR, rs, f32), ("dL", dL, rs, f32), ("dq", dq, qs, bf), ("dk", dk, ks, bf),
+                               ("dv", dv, ks, bf), ("dtau", dtau, rs, f32)):
+        if t is not None:
+            _plain(name, t, shape, dt)
+    _vector("seq_lens", seq_lens, B, torch.int32)
+    pd = PrefillDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, capacity_tokens=T,
+                     dtype=ETA_DT_BF16, beta=beta, additive=int(bool(additive)), C=C)
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check(lib.eta_gated_prefill_backward_workspace_size(ctypes.byref(pd), ctypes.byref(n)))
+    workspace = _workspace(workspace, n.value, dev)
+    with _On(dev, stream) as s:
+        _check(lib.eta_gated_prefill_backward(
+            ctypes.byref(pd), _ptr(q), _ptr(k), _ptr(v), _ptr(tau), _ptr(seq_lens), _ptr(out), _ptr(L),
+            _ptr(dout), _ptr(dR), _ptr(dL), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtau), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), s))
+    return dq, dk, dv, dtau

@@ -106,3 +106,52 @@ def test_binding_refuses_host_tensors():
         eta.qk_norm_rope_backward(x, x, None, x, x, freqs=None)
     with pytest.raises(TypeError):
         eta.qk_norm_rope(x.half(), x.half(), freqs=None)
+
+
+def prefill_desc(**kw):
+    d = dict(batch=2, num_q_heads=8, num_kv_heads=2, head_dim=128, capacity_tokens=100, dtype=eta.ETA_DT_BF16,
+             beta=4.0, additive=0, C=0.0)
+    d.update(kw)
+    return eta.PrefillDesc(**d)
+
+
+def prefill_grad(lib, desc=None, **kw):
+    a = dict(q=FAKE, k=FAKE, v=FAKE, tau=FAKE, lens=FAKE, out=FAKE, L=FAKE, dout=FAKE, dR=None, dL=None, dq=FAKE, dk=FAKE,
+             dv=FAKE, dtau=FAKE, ws=FAKE, bytes=1 << 30)
+    a.update(kw)
+    return lib.eta_gated_prefill_backward(None if desc == 0 else ctypes.byref(desc or prefill_desc()), *a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(batch=65536), INVALID), (dict(capacity_tokens=0), INVALID),
+    (dict(capacity_tokens=(1 << 24) + 1), UNSUPPORTED), (dict(num_kv_heads=3), INVALID),
+    (dict(num_q_heads=32), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(dtype=eta.ETA_DT_F32), UNSUPPORTED),
+    (dict(beta=-1.0), INVALID), (dict(beta=float("inf")), INVALID), (dict(additive=2), INVALID),
+    (dict(additive=1, C=float("nan")), INVALID)])
+def test_prefill_grad_descriptor_refused(lib, kw, code):
+    assert prefill_grad(lib, prefill_desc(**kw)) == code and lib.eta_last_error_string().decode()
+    n = ctypes.c_size_t()
+    assert lib.eta_gated_prefill_backward_workspace_size(ctypes.byref(prefill_desc(**kw)), ctypes.byref(n)) == code
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "tau", "lens", "out", "L", "dout", "dq", "dk", "dv", "dtau"])
+def test_prefill_grad_pointers_refused(lib, name):
+    assert prefill_grad(lib, **{name: None}) == INVALID
+    assert prefill_grad(lib, **{name: FAKE + 2}) == INVALID
+
+
+def test_prefill_grad_workspace_refused(lib):
+    n = ctypes.c_size_t()
+    assert lib.eta_gated_prefill_backward_workspace_size(ctypes.byref(prefill_desc()), ctypes.byref(n)) == eta.ETA_OK
+    assert n.value >= 4 * 2 * 8 * 100 * 4 and n.value % 256 == 0
+    assert prefill_grad(lib, ws=None) == WORKSPACE
+    assert prefill_grad(lib, ws=FAKE + 128) == WORKSPACE
+    assert prefill_grad(lib, bytes=n.value - 1) == WORKSPACE
+    assert prefill_grad(lib, dR=FAKE + 1) == INVALID and prefill_grad(lib, dL=FAKE + 2) == INVALID
+    assert prefill_grad(lib, 0) == INVALID
+
+
+def test_binding_refuses_prefill_tensors_on_the_host():
+    x, r = torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 3)
+    with pytest.raises(ValueError, match="GPU"):
+        eta.gated_prefill_backward(x, x, x, r, torch.zeros(1, dtype=torch.int32), x, r, x, beta=4.0)
