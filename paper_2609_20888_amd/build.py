@@ -40,7 +40,7 @@ def hipcc() -> str:
 # MFMA results kept in the ordinary vector registers: for the prefill kernel only
 # (no copies between accumulation and arithmetic registers there; the
 # calibration kernel is faster with the default register classes)
-VGPR_FORM = {"eta_prefill.hip", "eta_prefill_grad.hip"}
+VGPR_FORM = {"eta_prefill.hip"}
 
 
 def _flags(src: str):

@@ -37,7 +37,7 @@ struct GradArgs {
   const int32_t* seq_lens;
   uint16_t *dq, *dk, *dv;
   float* dtau;
-  float* stats;              // [4][B Hq][Tp]: -L and tau in base-2 units, -D, beta dR
+  float* stats;              // [4][B Hq][Tp]: -L', beta tau' + log2 is2, -D, beta dR
   float* part;               // [2][nsplit][B Hkv][T][d] partial dk, dv (nsplit > 1)
   int64_t stat_step;         // B Hq Tp
   int64_t part_step;         // nsplit B Hkv T d
@@ -54,7 +54,7 @@ extern "C" __device__ float eta_mul_legacy(float, float) __asm("llvm.amdgcn.fmul
 // = s2 sg, u E = 1 - sg, so sg' keeps its relative accuracy where the gate is nearly open or
 // nearly shut (the legacy product gives 0 for 0 x inf, the shut gate).
 struct Gate {
-  float s2, is2, nbs, lis2, kd, C2is;   // kd: beta / sqrt(d) (additive: beta C)
+  float s2, is2, nbs, lis2, kd, C2, C2is;   // kd: beta / sqrt(d) (additive: beta C)
   template <int D>
   static __device__ __forceinline__ Gate make(float beta, float C, bool add) {
     Gate g;
@@ -63,37 +63,77 @@ struct Gate {
     g.nbs = -beta * g.s2;
     g.lis2 = log2f(g.is2);
     g.kd = add ? beta * C : beta / sqrtf((float)D);
-    g.C2is = C * kLog2e * g.is2;
+    g.C2 = C * kLog2e;
+    g.C2is = g.C2 * g.is2;
     return g;
   }
 };
 
-// c: raw product, t: beta tau' + log2 is2, nl: -L' (additive: -L' - C'), dp: dO.v - D, kap: beta dR.
-// Gives P, s2 dS and s2 sg' m.
-template <bool ADD, bool MASKED>
-__device__ __forceinline__ void score_grad(const Gate& g, float c, float t, float nl, float nl_diag, float dp,
-                                           float kap, bool valid, bool diag, float& p, float& ds, float& n) {
-  const float e = __builtin_amdgcn_exp2f(fmaf(g.nbs, c, t));
-  const float u = __builtin_amdgcn_rcpf(e + g.is2);
-  const float w = u * eta_mul_legacy(u, e);
-  float y = ADD ? fmaf(g.C2is, u, fmaf(c, g.s2, nl)) : fmaf(c, u, nl);
-  if constexpr (MASKED) {
-    if (diag) y = fmaf(c, g.s2, nl_diag);
-    if (!valid) y = kNegInf;
-  }
-  p = __builtin_amdgcn_exp2f(y);
-  const float d = p * dp;
-  float m = fmaf(ADD ? d : d * c, g.kd, kap);
-  float lin = ADD ? g.s2 : u;
-  if constexpr (MASKED) {
-    if (diag) {
-      m = kap;
-      lin = g.s2;
+// The row scalars of a score: t: beta tau' + log2 is2; nl: -L'; kap: beta dR.
+struct RowScalars {
+  float t, nl, kap;
+};
+
+// The vector work of a unit: 16 scores of a lane, raw products in s and dO.v - D in dp, two
+// scores a step, the four stages of a score one step apart so that no step waits for its own
+// transcendentals; the last stage, the first to read dp, DL steps after the first.  row(j) gives score j's scalars, mask(j, valid, diag) its place (MASKED),
+// done(j, p, ds, n) takes P, s2 dS and s2 sg' m; beside(step) is the matrix work of a step.
+template <int DL, bool ADD, bool MASKED, typename Row, typename Mask, typename Done, typename Beside>
+__device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, const f32x16& dp, Row row, Mask mask,
+                                            Done done, Beside beside) {
+  float e[16], u[16], w[16], p[16];       // (a few of each are alive at a time)
+#pragma unroll
+  for (int st = 0; st < 8 + DL; ++st) {
+    beside(st);
+    if (st >= DL) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = 2 * (st - DL) + i, o = j;
+        const float d = p[o] * dp[j], kap = row(j).kap;
+        float m = fmaf(ADD ? d : d * s[j], g.kd, kap), lin = ADD ? g.s2 : u[o];
+        if constexpr (MASKED) {
+          bool valid, diag;
+          mask(j, valid, diag);
+          m = diag ? kap : m;
+          lin = diag ? g.s2 : lin;
+          m = valid ? m : 0.f;
+        }
+        const float n = w[o] * m;
+        done(j, p[o], fmaf(d, lin, n), n);
+      }
     }
-    if (!valid) m = 0.f;
+    if (st >= 2 && st < 10) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = 2 * (st - 2) + i, o = j;
+        w[o] = u[o] * eta_mul_legacy(u[o], e[o]);
+        const float nl = row(j).nl;
+        float y = ADD ? fmaf(g.C2is, u[o], fmaf(s[j], g.s2, nl - g.C2)) : fmaf(s[j], u[o], nl);
+        if constexpr (MASKED) {
+          bool valid, diag;
+          mask(j, valid, diag);
+          y = diag ? fmaf(s[j], g.s2, nl) : y;
+          y = valid ? y : kNegInf;
+        }
+        p[o] = __builtin_amdgcn_exp2f(y);
+      }
+    }
+    if (st >= 1 && st < 9) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int o = 2 * (st - 1) + i;
+        u[o] = __builtin_amdgcn_rcpf(e[o] + g.is2);
+      }
+    }
+    if (st < 8) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = 2 * st + i;
+        e[j] = __builtin_amdgcn_exp2f(fmaf(g.nbs, s[j], row(j).t));
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  n = w * m;
-  ds = fmaf(d, lin, n);
 }
 
 // The work of workgroup `wg` of nb blocks and NH (head, sequence) pairs: blocks in order of
@@ -112,75 +152,99 @@ __device__ __forceinline__ void grad_work(uint32_t wg, uint32_t H, uint32_t NH, 
   }
 }
 
-// Streams 64-row tiles of a [rows][D] tensor into swizzled LDS; rows from `rows` on repeat the
-// last one (what the tensor holds there, NaN too, must reach no product).
+// A 64-row tile of D bf16 in LDS: groups of 1 KiB (what a wavefront's direct load writes), 16 bytes
+// apart, and in a row the 16-byte chunks XORed by row, so that (a) the same chunk of 16
+// consecutive rows (row reads) and (b) an aligned run of four chunks of four consecutive rows
+// (transpose reads) both cover all 64 banks once.  The padding takes the part of the row that
+// would otherwise be XORed too: a lane's operands lie at four addresses plus constants.
+template <int D>
+struct Tile {
+  static constexpr int GR = 512 / D, GB = 1040;      // rows and bytes of a group
+  static constexpr int HALF = 32 / GR * GB, BYTES = 2 * HALF;
+  static constexpr int NR = 4;                       // row addresses of a lane
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (D == 128) return (row & 3) << 2;
+    return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1);
+  }
+  static __device__ __forceinline__ uint32_t at(int row, int chunk) {
+    return (uint32_t)(row / GR * GB + row % GR * 2 * D + 16 * (chunk ^ swizzle(row)));
+  }
+  // dims 16 kc + 8 (lane / 32) .. of row lane & 31: row_base(lane, kc / per) + row_step(kc)
+  static constexpr int PER = D / 16 / NR;
+  static __device__ __forceinline__ uint32_t row_base(int lane, int i) { return at(lane & 31, 2 * PER * i + (lane >> 5)); }
+  static constexpr int row_step(int kc) { return 32 * (kc % PER); }
+  // dims 32 db + (lane & 31) of rows 16 c + 8 hi + 4 (lane / 32) .. + 3: turn_base(lane, db) + turn_step(c, hi)
+  static __device__ __forceinline__ uint32_t turn_base(int lane, int db) {
+    const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    return at(row, chunk) + 8 * (lane & 1);
+  }
+  static constexpr int turn_step(int c, int hi) { return (16 * c + 8 * hi) / GR * GB; }
+};
+
+// Streams 64-row tiles of a [rows][D] tensor into LDS; rows from `rows` on repeat the last one
+// (what the tensor holds there, NaN too, must reach no product).
 template <int D>
 struct TileLoad {
   static constexpr int CPR = D / 8, NI = kGrT * CPR / 256, RPJ = 256 / CPR;
-  static_assert(RPJ % 16 == 0, "the swizzle takes row bits 0 .. 3");
+  static_assert(RPJ % 8 == 0, "the swizzle takes row bits 0 .. 2");
   int grow0;
   uint32_t goff;
   __device__ __forceinline__ explicit TileLoad(int tid)
-      : grow0(tid / CPR), goff((uint32_t)(grow0 * D + 8 * pf_chunk<D>(grow0, tid % CPR)) * 2u) {}
-  __device__ __forceinline__ void operator()(const uint16_t* src, uint16_t* tile, int w, int blk, int rows) const {
+      : grow0(tid / CPR), goff((uint32_t)(grow0 * D + 8 * ((tid % CPR) ^ Tile<D>::swizzle(grow0))) * 2u) {}
+  __device__ __forceinline__ void operator()(const uint16_t* src, char* tile, int w, int blk, int rows) const {
     const char* base = reinterpret_cast<const char*>(src + (int64_t)blk * kGrT * D);
-    uint16_t* dst = tile + 8 * 64 * w;
-    if ((blk + 1) * kGrT <= rows) {
+    char* dst = tile + w * Tile<D>::GB;
+    const bool whole = (blk + 1) * kGrT <= rows;
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
-        __builtin_amdgcn_global_load_lds((const void*)(base + goff + 4096 * j),
-                                         (__attribute__((address_space(3))) void*)(dst + 8 * 256 * j), 16, 0, 0);
-    } else {
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
+    for (int j = 0; j < NI; ++j) {
+      uint32_t off = goff + 4096u * j;
+      if (!whole) {
         const int row = RPJ * j + grow0;
-        const uint32_t off =
-            goff + 4096u * j - (uint32_t)(row - (min(blk * kGrT + row, rows - 1) - blk * kGrT)) * (2u * D);
-        __builtin_amdgcn_global_load_lds((const void*)(base + off),
-                                         (__attribute__((address_space(3))) void*)(dst + 8 * 256 * j), 16, 0, 0);
+        off -= (uint32_t)(row - (min(blk * kGrT + row, rows - 1) - blk * kGrT)) * (2u * D);
       }
+      __builtin_amdgcn_global_load_lds((const void*)(base + (int32_t)off),
+                                       (__attribute__((address_space(3))) void*)(dst + 4 * Tile<D>::GB * j), 16, 0, 0);
     }
   }
 };
 
-// Operands from a swizzled half tile (32 rows): rows as they are (row lane & 31, dims 16 kc + 8 g2 ..),
-// and transposed (dims 32 db + lane & 31 of the 16 rows of chunk c, in the order of pack_units).
-template <int D>
-struct TileRead {
-  int row_off, r32, g2, vt_row, vt_c, vt_half;
-  __device__ __forceinline__ explicit TileRead(int lane)
-      : r32(lane & 31), g2(lane >> 5), vt_row(4 * (lane >> 5) + ((lane & 15) >> 2)),
-        vt_c(2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)), vt_half(4 * (lane & 1)) {}
-  __device__ __forceinline__ u32x4 rows(const uint16_t* t, int kc) const {
-    return *reinterpret_cast<const u32x4*>(&t[r32 * D + 8 * pf_chunk<D>(r32, 2 * kc + g2)]);
-  }
-  __device__ __forceinline__ int off(int c, int db, int hi8) const {
-    const int row = vt_row + 8 * hi8;
-    return (16 * c + row) * D + 8 * pf_chunk<D>(row, 4 * db + vt_c) + vt_half;
-  }
-  __device__ __forceinline__ u32x4 turned(const uint16_t* t, int c, int db) const {
-    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) i16x4*)(&t[off(c, db, 0)]));
-    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) i16x4*)(&t[off(c, db, 1)]));
-    const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-    return u32x4{l2.x, l2.y, h2.x, h2.y};
-  }
-};
+typedef __attribute__((address_space(3))) char LdsBytes;
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(LdsBytes*)p; }
+__device__ __forceinline__ u32x4 lds_rows(uint32_t at) {
+  return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)at;
+}
+__device__ __forceinline__ f32x4 lds_floats(uint32_t at) {
+  return *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)at;
+}
+__device__ __forceinline__ u32x4 lds_turned(uint32_t lo, uint32_t hi) {
+  const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)lo);
+  const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)hi);
+  const uint2 a2 = __builtin_bit_cast(uint2, a), b2 = __builtin_bit_cast(uint2, b);
+  return u32x4{a2.x, a2.y, b2.x, b2.y};
+}
 
 __device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
                                                  0, 0, 0);
 }
 
-// A unit's 16 values of a lane as the two B operands of a product over the unit's 32 rows
-__device__ __forceinline__ void pack_units(const float (&x)[16], u32x4 (&o)[2]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o[i >> 1][2 * (i & 1)] = pack_bf16x2(x[4 * i], x[4 * i + 1]);
-    o[i >> 1][2 * (i & 1) + 1] = pack_bf16x2(x[4 * i + 2], x[4 * i + 3]);
+// A unit's 16 values of a lane, given in order, as the two B operands of a product over the
+// unit's 32 rows (bf16 pairs).
+struct Packer {
+  u32x4 o[2];
+  float hold;
+  __device__ __forceinline__ void put(int j, float x) {
+    if (j & 1) {
+      // (taken here: the work behind it is otherwise moved to where the pair is used, a unit
+      // later, and its operands stay in registers)
+      uint32_t both = pack_bf16x2(hold, x);
+      asm volatile("" : "+v"(both));
+      o[j >> 3][(j >> 1) & 3] = both;
+    } else {
+      hold = x;
+    }
   }
-}
+};
 
 __device__ __forceinline__ float dot_bf16(const u32x4& a, const u32x4& b, float s) {
 #pragma unroll
@@ -197,8 +261,8 @@ __device__ __forceinline__ float dot_bf16(const u32x4& a, const u32x4& b, float 
 template <int D, bool ADD>
 __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
   constexpr int KC = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(16))) uint16_t k_s[2][kGrT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t v_s[2][kGrT * D];
+  using TL = Tile<D>;
+  __shared__ __attribute__((aligned(16))) char lds[2][2 * TL::BYTES];        // K, V
   const uint32_t nqb = gridDim.x, NH = gridDim.y * gridDim.z;
   int blk, h, b;
   grad_work(blockIdx.x + nqb * (blockIdx.y + gridDim.y * blockIdx.z), (uint32_t)a.Hq, NH, blk, h, b);
@@ -222,10 +286,10 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
   }
   // row scalars; rows at or past the sequence's end take P = 0 and no gradient
   const bool in = t < Tb;
-  float nl = kNegInf, bt = 0.f, nd = 0.f, kap = 0.f;
+  float nl = kNegInf, bt = g.lis2, nd = 0.f, kap = 0.f;
   if (in) {
     nl = -a.L[qrow0 + t] * kLog2e;
-    bt = a.beta * a.tau[qrow0 + t] * kLog2e;
+    bt = fmaf(a.beta * kLog2e, a.tau[qrow0 + t], g.lis2);
     nd = -row2_sum(dsum);
     if (a.dL) nd += a.dL[qrow0 + t];
     if (a.dR) kap = a.beta * a.dR[qrow0 + t];
@@ -237,10 +301,13 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
     st[2 * a.stat_step] = nd;
     st[3 * a.stat_step] = kap;
   }
-  const float nlg = ADD ? nl - a.C * kLog2e : nl, btl = bt + g.lis2;
 
   const TileLoad<D> load(tid);
-  const TileRead<D> rd(lane);
+  uint32_t ra[TL::NR], ta[DB];
+#pragma unroll
+  for (int i = 0; i < TL::NR; ++i) ra[i] = lds_address(lds[0]) + TL::row_base(lane, i);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds[0]) + TL::turn_base(lane, db);
   const uint16_t *kh = a.k + kvoff, *vh = a.v + kvoff;
   const int last_row = min(qblk * kGrQ + kGrQ, Tb) - 1;
   const int nkb = last_row >= qblk * kGrQ ? last_row / kGrT + 1 : 0;
@@ -249,49 +316,91 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = f32x16{};
   float nsum = 0.f;
+  const RowScalars rs{bt, nl, kap};
 
-  auto unit = [&](int u, const uint16_t* kt, const uint16_t* vt, auto masked_tag) {
+  // One unit of 32 keys: the score products, the vector work, the product into dq.  Nothing of a
+  // wavefront overlaps with its own vector work; the other wavefront of the SIMD's does.
+  constexpr int LA = 4;                              // LDS operands ahead of their MFMA
+  auto unit = [&](int u, int kt, auto masked_tag) {      // kt: byte offset of the unit's keys
     constexpr bool MASKED = decltype(masked_tag)::value;
+    u32x4 op[LA];
     f32x16 s{}, dp;
 #pragma unroll
     for (int i = 0; i < 16; ++i) dp[i] = nd;
+    auto rd = [&](int x) {
+      if (x < 2 * KC)
+        op[x % LA] = lds_rows(ra[(x >> 1) / TL::PER] + kt + (x & 1 ? TL::BYTES : 0) + TL::row_step(x >> 1));
+    };
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) s = mfma(rd.rows(kt, kc), qb[kc], s);
+    for (int x = 0; x < LA; ++x) rd(x);
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) dp = mfma(rd.rows(vt, kc), dob[kc], dp);
-    float ds[16], un = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int j = u * 32 + 8 * (i >> 2) + 4 * g2 + (i & 3);
-      float p, n;
-      score_grad<ADD, MASKED>(g, s[i], btl, nlg, nl, dp[i], kap, j <= t && in, j == t, p, ds[i], n);
-      un += n;
+    for (int x = 0; x < 2 * KC; ++x) {
+      if (x & 1) dp = mfma(op[x % LA], dob[x >> 1], dp);
+      else s = mfma(op[x % LA], qb[x >> 1], s);
+      rd(x + LA);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    Packer pk;
+    float un = 0.f;
+    unit_scores<3, ADD, MASKED>(
+        g, s, dp, [&](int) { return rs; },
+        [&](int i, bool& valid, bool& diag) {
+          const int j = u * 32 + 8 * (i >> 2) + 4 * g2 + (i & 3);
+          valid = j <= t && in;
+          diag = j == t;
+        },
+        [&](int i, float, float ds, float n) {
+          pk.put(i, ds);
+          un += n;
+          if (i & 1) asm volatile("" : "+v"(un));
+        },
+        [](int) {});
     nsum += un;
-    u32x4 x[2];
-    pack_units(ds, x);
+    auto rt = [&](int x) {
+      if (x < 2 * DB)
+        op[x % LA] = lds_turned(ta[x % DB] + kt + TL::turn_step(x / DB, 0), ta[x % DB] + kt + TL::turn_step(x / DB, 1));
+    };
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int x = 0; x < LA; ++x) rt(x);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) acc[db] = mfma(rd.turned(kt, c, db), x[c], acc[db]);
+    for (int x = 0; x < 2 * DB; ++x) {
+      acc[x % DB] = mfma(op[x % LA], pk.o[x / DB], acc[x % DB]);
+      rt(x + LA);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
-  if (nkb > 0) {
-    load(kh, k_s[0], w, 0, Tb);
-    load(vh, v_s[0], w, 0, Tb);
-  }
-  for (int kb = 0; kb < nkb; ++kb) {
+  // Blocks of 64 keys, two buffers: at the start of a block its tiles have arrived (the barrier says
+  // so for every wavefront's part) and every wavefront is done with the other buffer.
+  auto arrive = [&](int kb, int buf) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (kb + 1 < nkb) {
-      load(kh, k_s[(kb + 1) & 1], w, kb + 1, Tb);
-      load(vh, v_s[(kb + 1) & 1], w, kb + 1, Tb);
+      load(kh, lds[buf ^ 1], w, kb + 1, Tb);
+      load(vh, lds[buf ^ 1] + TL::BYTES, w, kb + 1, Tb);
+    }
+  };
+  if (nkb > 0) {
+    load(kh, lds[0], w, 0, Tb);
+    load(vh, lds[0] + TL::BYTES, w, 0, Tb);
+    constexpr std::integral_constant<bool, false> plain{};
+    constexpr std::integral_constant<bool, true> masked{};
+    // the blocks before the workgroup's rows (an even number of them) need no mask
+    for (int kb = 0; kb < 2 * qblk; kb += 2) {
+#pragma unroll
+      for (int buf = 0; buf < 2; ++buf) {
+        arrive(kb + buf, buf);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          unit(2 * (kb + buf) + x, buf * 2 * TL::BYTES + x * TL::HALF, plain);
+      }
     }
 #pragma unroll 1
-    for (int u = 2 * kb; u < min(2 * kb + 2, nu); ++u) {
-      const uint16_t *kt = k_s[kb & 1] + (u & 1) * 32 * D, *vt = v_s[kb & 1] + (u & 1) * 32 * D;
-      if (u < nu - 1) unit(u, kt, vt, std::integral_constant<bool, false>{});
-      else unit(u, kt, vt, std::integral_constant<bool, true>{});
+    for (int kb = 2 * qblk; kb < nkb; ++kb) {
+      arrive(kb, kb & 1);
+#pragma unroll 1
+      for (int u = 2 * kb; u < min(2 * kb + 2, nu); ++u)
+        unit(u, (kb & 1) * 2 * TL::BYTES + (u & 1) * TL::HALF, masked);
     }
   }
 
@@ -314,12 +423,16 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
 // lane's own P and dS (bf16) as B and dO^T, Q^T from transpose reads.  The tiles run from the
 // sequence's end down to the keys' own rows, so that the workgroups of one kv head, which start
 // together, read the same tiles at the same time.
+//
+// At d = 128 the sums take 128 registers and the keys 64, so one wavefront runs on a SIMD and the
+// overlap is made inside it: beside the vector work of a unit (32 query rows) run the products of
+// the unit before into dv and dk and the score products of the unit after.
 template <int D, bool ADD>
-__global__ __launch_bounds__(256, 1) void grad_kv_kernel(GradArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void grad_kv_kernel(GradArgs a) {
   constexpr int KC = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(16))) uint16_t q_s[2][kGrT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t do_s[2][kGrT * D];
-  __shared__ __attribute__((aligned(16))) float st_s[2][4][kGrT];
+  using TL = Tile<D>;
+  constexpr int TILE = TL::BYTES, HALF = TL::HALF, BUF = 2 * TILE + 4 * kGrT * 4;      // bytes
+  __shared__ __attribute__((aligned(16))) char lds[3][BUF];        // Q, dO, row scalars
   const uint32_t NH = gridDim.y * gridDim.z;
   int kblk, hs, b;
   grad_work(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), (uint32_t)gridDim.y, NH, kblk, hs, b);
@@ -343,74 +456,191 @@ __global__ __launch_bounds__(256, 1) void grad_kv_kernel(GradArgs a) {
   for (int db = 0; db < DB; ++db) dka[db] = dva[db] = f32x16{};
 
   const TileLoad<D> load(tid);
-  const TileRead<D> rd(lane);
-  // tiles of 64 query rows of a head: from nqb - 1 down to qb0; units from the wavefront's own (ku) on
-  const int qb0 = kblk * (kGrQ / kGrT), nqb = (Tb + kGrT - 1) / kGrT, nb = max(nqb - qb0, 0);
-  const int ku = wrow0 / 32, steps = nb * GH;
+  // Tiles of 64 query rows: of each head from the pair that holds the sequence's last row (its rows
+  // past the end have P = 0) down to the pair of the keys' own rows.
+  const int nqb = 2 * ((Tb + kGrQ - 1) / kGrQ), nb = max(nqb - 2 * kblk, 0), steps = nb * GH;
+  const int ku = wrow0 / 32;                                   // the unit of the wavefront's diagonal
 
-  auto fetch = [&](int it, int buf) {
-    const int hh = it / nb, qb = nqb - 1 - (it - hh * nb);
-    const int64_t head = (int64_t)b * a.Hq + h0 + hh;
-    load(a.q + head * a.T * D, q_s[buf], w, qb, Tb);
-    load(a.dout + head * a.T * D, do_s[buf], w, qb, Tb);
+  int fh = 0, fq = nqb - 1;                                    // next tile to fetch
+  auto fetch = [&](int buf) {
+    const int64_t head = (int64_t)b * a.Hq + h0 + fh;
+    load(a.q + head * a.T * D, lds[buf], w, fq, Tb);
+    load(a.dout + head * a.T * D, lds[buf] + TILE, w, fq, Tb);
     if (w == 0)      // lane l: four rows of scalar l / 16
       __builtin_amdgcn_global_load_lds(
-          (const void*)(a.stats + (lane >> 4) * a.stat_step + head * a.Tp + qb * kGrT + 4 * (lane & 15)),
-          (__attribute__((address_space(3))) void*)&st_s[buf][0][0], 16, 0, 0);
-  };
-  auto unit = [&](int row0, const uint16_t* qt, const uint16_t* dt, const float* st, auto masked_tag) {
-    constexpr bool MASKED = decltype(masked_tag)::value;
-    f32x16 s{}, dp;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const f32x4 nd = *reinterpret_cast<const f32x4*>(st + 2 * kGrT + 8 * x + 4 * g2);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) dp[4 * x + i] = nd[i];
+          (const void*)(a.stats + (lane >> 4) * a.stat_step + head * a.Tp + fq * kGrT + 4 * (lane & 15)),
+          (__attribute__((address_space(3))) void*)&lds[buf][2 * TILE], 16, 0, 0);
+    if (fq-- == 2 * kblk) {
+      fq = nqb - 1;
+      ++fh;
     }
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc) s = mfma(rd.rows(qt, kc), kf[kc], s);
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc) dp = mfma(rd.rows(dt, kc), vf[kc], dp);
-    float p[16], ds[16];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const f32x4 nl = *reinterpret_cast<const f32x4*>(st + 8 * x + 4 * g2);
-      const f32x4 bt = *reinterpret_cast<const f32x4*>(st + kGrT + 8 * x + 4 * g2);
-      const f32x4 kap = *reinterpret_cast<const f32x4*>(st + 3 * kGrT + 8 * x + 4 * g2);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = row0 + 8 * x + 4 * g2 + i;
-        float n;
-        score_grad<ADD, MASKED>(g, s[4 * x + i], bt[i] + g.lis2, ADD ? nl[i] - a.C * kLog2e : nl[i], nl[i],
-                                dp[4 * x + i], kap[i], j <= row, j == row, p[4 * x + i], ds[4 * x + i], n);
-      }
-    }
-    u32x4 pp[2], pd[2];
-    pack_units(p, pp);
-    pack_units(ds, pd);
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        dva[db] = mfma(rd.turned(dt, c, db), pp[c], dva[db]);
-        dka[db] = mfma(rd.turned(qt, c, db), pd[c], dka[db]);
-      }
   };
 
-  if (steps > 0) fetch(0, 0);
-  for (int it = 0; it < steps; ++it) {
+  // Operand addresses: Q rows of the tile whose scores come next (ra), dO rows (da) and scalars (sa)
+  // of the unit's own, transposed rows of the tile whose products are due (ta).
+  uint32_t ra[TL::NR], da[TL::NR], ta[DB], sa = lds_address(lds[0]) + 2 * TILE + 16 * g2;
+#pragma unroll
+  for (int i = 0; i < TL::NR; ++i) {
+    ra[i] = lds_address(lds[0]) + TL::row_base(lane, i);
+    da[i] = ra[i] + TILE;
+  }
+#pragma unroll
+  for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds[0]) + TL::turn_base(lane, db);
+  auto scalars = [&](int which, int half, int x) {             // rows 8 x + 4 g2 .. + 3 of a half tile
+    return lds_floats(sa + which * 4 * kGrT + half * 128 + 32 * x);
+  };
+
+  // MFMAs beside a unit (half H of its tile): its own dP, which its last stage reads, the products of
+  // the unit before, the raw scores of the unit after.  LDS operands are read LA MFMAs ahead.
+  constexpr int NP = 4 * DB, NT = 2 * KC + NP, LA = 4;
+  constexpr int DL = 5, ST = 8 + DL;
+  u32x4 pp[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}, pd[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
+  u32x4 op[LA];
+  f32x16 dp;
+  auto rd = [&](int x, int half) {
+    if (x < KC) {
+      op[x % LA] = lds_rows(da[x / TL::PER] + half * HALF + TL::row_step(x));
+    } else if (x < KC + NP) {
+      const int y = x - KC, c = y / (2 * DB), db = y % (2 * DB) / 2;
+      const int o = (y & 1 ? 0 : TILE) + (half ^ 1) * HALF;
+      op[x % LA] = lds_turned(ta[db] + o + TL::turn_step(c, 0), ta[db] + o + TL::turn_step(c, 1));
+    } else if (x < NT) {
+      const int kc = x - KC - NP;
+      op[x % LA] = lds_rows(ra[kc / TL::PER] + (half ^ 1) * HALF + TL::row_step(kc));
+    }
+  };
+  auto step = [&](int x, f32x16& sn) {
+    if (x < KC) {
+      dp = mfma(op[x % LA], vf[x], dp);
+    } else if (x < KC + NP) {
+      const int y = x - KC, c = y / (2 * DB), db = y % (2 * DB) / 2;
+      if (y & 1) dka[db] = mfma(op[x % LA], pd[c], dka[db]);
+      else dva[db] = mfma(op[x % LA], pp[c], dva[db]);
+    } else {
+      sn = mfma(op[x % LA], kf[x - KC - NP], sn);
+    }
+  };
+
+  // One unit, its raw scores in s; those of the next are left in sn.  MODE 0: every key precedes
+  // every row; 1: the diagonal; 2: no pair of the unit counts.
+  auto unit = [&](int row0, f32x16& s, f32x16& sn, auto half_tag, auto mode_tag) {
+    constexpr int H = decltype(half_tag)::value, MODE = decltype(mode_tag)::value;
+    sn = f32x16{};
+    Packer kp, kd;
+    if constexpr (MODE == 2) {
+#pragma unroll
+      for (int x = KC; x < KC + LA; ++x) rd(x, H);
+#pragma unroll
+      for (int x = KC; x < NT; ++x) {
+        step(x, sn);
+        rd(x + LA, H);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) kp.o[i] = kd.o[i] = u32x4{0, 0, 0, 0};
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const f32x4 nd = scalars(2, H, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dp[4 * x + i] = nd[i];
+      }
+#pragma unroll
+      for (int x = 0; x < LA; ++x) rd(x, H);
+      f32x4 nl[4], bt[4], kap[4];
+      bt[0] = scalars(1, H, 0);
+      unit_scores<DL, ADD, MODE == 1>(
+          g, s, dp,
+          [&](int i) {
+            return RowScalars{bt[i >> 2][i & 3], nl[i >> 2][i & 3], kap[i >> 2][i & 3]};
+          },
+          [&](int i, bool& valid, bool& diag) {
+            const int row = row0 + 8 * (i >> 2) + 4 * g2 + (i & 3);
+            valid = j <= row;
+            diag = j == row;
+          },
+          [&](int i, float p, float ds, float) {
+            kp.put(i, p);
+            kd.put(i, ds);
+          },
+          [&](int st) {
+            // the scalars of four rows are read a step before the first of them is due
+            if (st % 2 == 1 && st < 7) bt[(st + 1) / 2] = scalars(1, H, (st + 1) / 2);
+            if (st % 2 == 1 && st < 8) nl[st / 2] = scalars(0, H, st / 2);
+            if (st >= DL - 1 && (st - DL + 1) % 2 == 0 && st < DL + 7) kap[(st - DL + 1) / 2] = scalars(3, H, (st - DL + 1) / 2);
+#pragma unroll
+            for (int x = 0; x < NT; ++x)
+              if ((x < KC ? x * (DL - 1) / KC : DL - 1 + (x - KC) * (ST - DL + 1) / (NT - KC)) == st) {
+                step(x, sn);
+                rd(x + LA, H);
+              }
+          });
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      pp[i] = kp.o[i];
+      pd[i] = kd.o[i];
+    }
+  };
+
+  if (steps > 0) {
+    constexpr std::integral_constant<int, 0> c0{};
+    constexpr std::integral_constant<int, 1> c1{};
+    constexpr std::integral_constant<int, 2> c2{};
+    fetch(0);
+    if (steps > 1) fetch(1);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (it + 1 < steps) fetch(it + 1, (it + 1) & 1);
-    const int qb = nqb - 1 - it % nb, buf = it & 1;
+    f32x16 s0, s1{};
+    // (the products before the first unit are of zeros with tile 0's rows)
+#pragma unroll
+    for (int x = 0; x < KC; ++x) s1 = mfma(lds_rows(ra[x / TL::PER] + HALF + TL::row_step(x)), kf[x], s1);
+    // Tile `it` (buffer it % 3): its upper half beside the tile before, then its lower half beside the
+    // tile after.  In between tile it + 1 has arrived and the buffer of tile it - 1 is free.
+    int buf = 0, it = 0;
+    auto between = [&] {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (it + 2 < steps) fetch(buf == 0 ? 2 : buf - 1);
+      const uint32_t on = buf == 2 ? -2u * BUF : (uint32_t)BUF, was = buf == 0 ? -2u * BUF : (uint32_t)BUF;
+      if (it > 0)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) ta[db] += was;
+      if (it + 1 < steps)
+#pragma unroll
+        for (int i = 0; i < TL::NR; ++i) ra[i] += on;
+    };
+    auto after = [&] {
+      const uint32_t on = buf == 2 ? -2u * BUF : (uint32_t)BUF;
+#pragma unroll
+      for (int i = 0; i < TL::NR; ++i) da[i] += on;
+      sa += on;
+      buf = buf == 2 ? 0 : buf + 1;
+      ++it;
+    };
+    for (int hh = 0; hh < GH; ++hh) {
 #pragma unroll 1
-    for (int x = 0; x < 2; ++x) {
-      const int u = 2 * qb + x;
-      if (u < ku) continue;
-      const uint16_t *qt = q_s[buf] + x * 32 * D, *dt = do_s[buf] + x * 32 * D;
-      const float* st = &st_s[buf][0][32 * x];
-      if (u == ku) unit(32 * u, qt, dt, st, std::integral_constant<bool, true>{});
-      else unit(32 * u, qt, dt, st, std::integral_constant<bool, false>{});
+      for (int qb = nqb - 1; qb > 2 * kblk + 1; --qb) {
+        unit(qb * kGrT + 32, s1, s0, c1, c0);
+        between();
+        unit(qb * kGrT, s0, s1, c0, c0);
+        after();
+      }
+#pragma unroll 1
+      for (int qb = 2 * kblk + 1; qb >= 2 * kblk; --qb) {
+        if (2 * qb + 1 >= ku) unit(qb * kGrT + 32, s1, s0, c1, c1);
+        else unit(qb * kGrT + 32, s1, s0, c1, c2);
+        between();
+        if (2 * qb >= ku) unit(qb * kGrT, s0, s1, c0, c1);
+        else unit(qb * kGrT, s0, s1, c0, c2);
+        after();
+      }
+    }
+    // the last unit's products: turned rows of the last tile's lower half
+#pragma unroll
+    for (int x = KC; x < KC + NP; ++x) {
+      rd(x, 1);
+      step(x, s0);
     }
   }
 
