@@ -37,9 +37,8 @@ struct GradArgs {
   const int32_t* seq_lens;
   uint16_t *dq, *dk, *dv;
   float* dtau;
-  float* stats;              // [4][B Hq][Tp]: -L', beta tau' + log2 is2, -D, beta dR
+  float* stats;              // [B Hq][Tp / 32][4][32]: -L', beta tau' + log2 is2, -D, beta dR
   float* part;               // [2][nsplit][B Hkv][T][d] partial dk, dv (nsplit > 1)
-  int64_t stat_step;         // B Hq Tp
   int64_t part_step;         // nsplit B Hkv T d
   int Hq, Hkv, T, Tp, nsplit;
   float beta, C;
@@ -152,7 +151,7 @@ __device__ __forceinline__ void grad_work(uint32_t wg, uint32_t H, uint32_t NH, 
   }
 }
 
-// A 64-row tile of D bf16 in LDS: groups of 1 KiB (what a wavefront's direct load writes), 16 bytes
+// A tile of rows of D bf16 in LDS: groups of 1 KiB (what a wavefront's direct load writes), 16 bytes
 // apart, and in a row the 16-byte chunks XORed by row, so that (a) the same chunk of 16
 // consecutive rows (row reads) and (b) an aligned run of four chunks of four consecutive rows
 // (transpose reads) both cover all 64 banks once.  The padding takes the part of the row that
@@ -160,7 +159,7 @@ __device__ __forceinline__ void grad_work(uint32_t wg, uint32_t H, uint32_t NH, 
 template <int D>
 struct Tile {
   static constexpr int GR = 512 / D, GB = 1040;      // rows and bytes of a group
-  static constexpr int HALF = 32 / GR * GB, BYTES = 2 * HALF;
+  static constexpr int HALF = 32 / GR * GB, BYTES = 2 * HALF;   // of 32 and 64 rows
   static constexpr int NR = 4;                       // row addresses of a lane
   static __device__ __forceinline__ int swizzle(int row) {
     if constexpr (D == 128) return (row & 3) << 2;
@@ -181,28 +180,25 @@ struct Tile {
   static constexpr int turn_step(int c, int hi) { return (16 * c + 8 * hi) / GR * GB; }
 };
 
-// Streams 64-row tiles of a [rows][D] tensor into LDS; rows from `rows` on repeat the last one
+// Streams tiles of R rows of a [rows][D] tensor into LDS; rows from `rows` on repeat the last one
 // (what the tensor holds there, NaN too, must reach no product).
-template <int D>
+template <int D, int R = kGrT>
 struct TileLoad {
-  static constexpr int CPR = D / 8, NI = kGrT * CPR / 256, RPJ = 256 / CPR;
+  static constexpr int CPR = D / 8, NI = R * CPR / 256, RPJ = 256 / CPR;
   static_assert(RPJ % 8 == 0, "the swizzle takes row bits 0 .. 2");
   int grow0;
   uint32_t goff;
   __device__ __forceinline__ explicit TileLoad(int tid)
       : grow0(tid / CPR), goff((uint32_t)(grow0 * D + 8 * ((tid % CPR) ^ Tile<D>::swizzle(grow0))) * 2u) {}
   __device__ __forceinline__ void operator()(const uint16_t* src, char* tile, int w, int blk, int rows) const {
-    const char* base = reinterpret_cast<const char*>(src + (int64_t)blk * kGrT * D);
+    const int row0 = min(blk * R, rows - 1), over = blk * R + R - rows;
+    const char* base = reinterpret_cast<const char*>(src + (int64_t)row0 * D);
     char* dst = tile + w * Tile<D>::GB;
-    const bool whole = (blk + 1) * kGrT <= rows;
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       uint32_t off = goff + 4096u * j;
-      if (!whole) {
-        const int row = RPJ * j + grow0;
-        off -= (uint32_t)(row - (min(blk * kGrT + row, rows - 1) - blk * kGrT)) * (2u * D);
-      }
-      __builtin_amdgcn_global_load_lds((const void*)(base + (int32_t)off),
+      if (over > 0) off -= (uint32_t)max(RPJ * j + grow0 - (rows - 1 - row0), 0) * (2u * D);
+      __builtin_amdgcn_global_load_lds((const void*)(base + off),
                                        (__attribute__((address_space(3))) void*)(dst + 4 * Tile<D>::GB * j), 16, 0, 0);
     }
   }
@@ -295,11 +291,11 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
     if (a.dR) kap = a.beta * a.dR[qrow0 + t];
   }
   if (g2 == 0) {
-    float* st = a.stats + head * a.Tp + t;
+    float* st = a.stats + (head * a.Tp + wrow0) * 4 + r32;
     st[0] = nl;
-    st[a.stat_step] = bt;
-    st[2 * a.stat_step] = nd;
-    st[3 * a.stat_step] = kap;
+    st[32] = bt;
+    st[64] = nd;
+    st[96] = kap;
   }
 
   const TileLoad<D> load(tid);
@@ -419,20 +415,24 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
 }
 
 // dk, dv of 128 keys: each lane owns a key.  S = Q K^T and dP = dO V^T - D with A from LDS (rows of
-// Q and dO) and B the wavefront's keys in registers; dv^T += dO^T P and dk^T += Q^T dS with the
-// lane's own P and dS (bf16) as B and dO^T, Q^T from transpose reads.  The tiles run from the
-// sequence's end down to the keys' own rows, so that the workgroups of one kv head, which start
-// together, read the same tiles at the same time.
+// Q and dO) and B the wavefront's keys; dv^T += dO^T P and dk^T += Q^T dS with the lane's own P and
+// dS (bf16) as B and dO^T, Q^T from transpose reads.  The tiles run from the sequence's end down to
+// the keys' own rows, so that the workgroups of one kv head, which start together, read the same
+// tiles at the same time.
 //
-// At d = 128 the sums take 128 registers and the keys 64, so one wavefront runs on a SIMD and the
-// overlap is made inside it: beside the vector work of a unit (32 query rows) run the products of
-// the unit before into dv and dk and the score products of the unit after.
+// At d = 128 the sums take 128 registers; V stays in LDS (a B operand read each time), so that two
+// wavefronts fit a SIMD and the matrix work of one runs beside the vector work of the other.
+// (With V in registers too only one fits: 3.2K cycles a unit with all its matrix work threaded
+// through the vector work, a quarter of them waits.)
 template <int D, bool ADD>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void grad_kv_kernel(GradArgs a) {
+__global__ __launch_bounds__(256, 2) void grad_kv_kernel(GradArgs a) {
   constexpr int KC = D / 16, DB = D / 32;
+  constexpr bool VLDS = D == 128;
+  constexpr int TR = D == 128 ? 32 : 64, UT = TR / 32;             // rows and units of a tile
   using TL = Tile<D>;
-  constexpr int TILE = TL::BYTES, HALF = TL::HALF, BUF = 2 * TILE + 4 * kGrT * 4;      // bytes
-  __shared__ __attribute__((aligned(16))) char lds[3][BUF];        // Q, dO, row scalars
+  constexpr int TILE = UT * TL::HALF, BUF = 2 * TILE + 4 * TR * 4, NKL = VLDS ? 2 : 0;
+  constexpr int VB = VLDS ? 4 * (KC + NKL) * 1024 : 0;             // bytes
+  __shared__ __attribute__((aligned(16))) char lds[VB + 2 * BUF];  // V (and two operands of K), then twice: Q, dO, row scalars
   const uint32_t NH = gridDim.y * gridDim.z;
   int kblk, hs, b;
   grad_work(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), (uint32_t)gridDim.y, NH, kblk, hs, b);
@@ -444,203 +444,150 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void grad_kv_kernel(GradArgs 
   const Gate g = Gate::make<D>(a.beta, a.C, ADD);
   const int wrow0 = kblk * kGrQ + 32 * w, j = wrow0 + r32, jk = min(j, max(Tb, 1) - 1);
   const int64_t kvrow0 = ((int64_t)b * a.Hkv + kvh) * a.T;
-  u32x4 kf[KC], vf[KC];
+  u32x4 kf[KC - NKL], vf[VLDS ? 1 : KC];
+  const uint32_t va = lds_address(lds) + w * (KC + NKL) * 1024 + lane * 16;   // operands of 1 KiB, as they are read
 #pragma unroll
   for (int kc = 0; kc < KC; ++kc) {
     const int64_t at = (kvrow0 + jk) * D + 16 * kc + 8 * g2;
-    kf[kc] = *reinterpret_cast<const u32x4*>(a.k + at);
-    vf[kc] = *reinterpret_cast<const u32x4*>(a.v + at);
+    const u32x4 kk = *reinterpret_cast<const u32x4*>(a.k + at), vv = *reinterpret_cast<const u32x4*>(a.v + at);
+    auto put = [&](int n, const u32x4& x) { *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(va + n * 1024) = x; };
+    if (kc < NKL) put(KC + kc, kk);
+    else kf[kc - NKL] = kk;
+    if constexpr (VLDS) put(kc, vv);
+    else vf[kc] = vv;
   }
   f32x16 dka[DB], dva[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dka[db] = dva[db] = f32x16{};
 
-  const TileLoad<D> load(tid);
-  // Tiles of 64 query rows: of each head from the pair that holds the sequence's last row (its rows
-  // past the end have P = 0) down to the pair of the keys' own rows.
-  const int nqb = 2 * ((Tb + kGrQ - 1) / kGrQ), nb = max(nqb - 2 * kblk, 0), steps = nb * GH;
-  const int ku = wrow0 / 32;                                   // the unit of the wavefront's diagonal
-
-  int fh = 0, fq = nqb - 1;                                    // next tile to fetch
+  // Tiles of each head: from the pair of tiles that holds the sequence's last row (rows past the end
+  // have P = 0) down to the keys' own rows, an even number of them.
+  const TileLoad<D, TR> load(tid);
+  const int t0 = kblk * (kGrQ / TR), nt = 2 * ((Tb + 2 * TR - 1) / (2 * TR)), nb = max(nt - t0, 0), steps = nb * GH;
+  const int ku = wrow0 / 32;                                       // the unit of the wavefront's diagonal
+  int fh = 0, ft = nt - 1;                                         // next tile to fetch
   auto fetch = [&](int buf) {
     const int64_t head = (int64_t)b * a.Hq + h0 + fh;
-    load(a.q + head * a.T * D, lds[buf], w, fq, Tb);
-    load(a.dout + head * a.T * D, lds[buf] + TILE, w, fq, Tb);
-    if (w == 0)      // lane l: four rows of scalar l / 16
-      __builtin_amdgcn_global_load_lds(
-          (const void*)(a.stats + (lane >> 4) * a.stat_step + head * a.Tp + fq * kGrT + 4 * (lane & 15)),
-          (__attribute__((address_space(3))) void*)&lds[buf][2 * TILE], 16, 0, 0);
-    if (fq-- == 2 * kblk) {
-      fq = nqb - 1;
+    char* dst = lds + VB + buf * BUF;
+    load(a.q + head * a.T * D, dst, w, ft, Tb);
+    load(a.dout + head * a.T * D, dst + TILE, w, ft, Tb);
+    if (w < 4 * TR / 64)                                           // 64 of the 4 TR scalars
+      __builtin_amdgcn_global_load_lds((const void*)(a.stats + (head * a.Tp + ft * TR) * 4 + tid),
+                                       (__attribute__((address_space(3))) void*)(dst + 2 * TILE + 256 * w), 4, 0, 0);
+    if (ft-- == t0) {
+      ft = nt - 1;
       ++fh;
     }
   };
 
-  // Operand addresses: Q rows of the tile whose scores come next (ra), dO rows (da) and scalars (sa)
-  // of the unit's own, transposed rows of the tile whose products are due (ta).
-  uint32_t ra[TL::NR], da[TL::NR], ta[DB], sa = lds_address(lds[0]) + 2 * TILE + 16 * g2;
+  uint32_t ra[TL::NR], ta[DB];
 #pragma unroll
-  for (int i = 0; i < TL::NR; ++i) {
-    ra[i] = lds_address(lds[0]) + TL::row_base(lane, i);
-    da[i] = ra[i] + TILE;
-  }
+  for (int i = 0; i < TL::NR; ++i) ra[i] = lds_address(lds) + VB + TL::row_base(lane, i);
 #pragma unroll
-  for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds[0]) + TL::turn_base(lane, db);
-  auto scalars = [&](int which, int half, int x) {             // rows 8 x + 4 g2 .. + 3 of a half tile
-    return lds_floats(sa + which * 4 * kGrT + half * 128 + 32 * x);
-  };
+  for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds) + VB + TL::turn_base(lane, db);
+  const uint32_t sa = lds_address(lds) + VB + 2 * TILE + 16 * g2;
 
-  // MFMAs beside a unit (half H of its tile): its own dP, which its last stage reads, the products of
-  // the unit before, the raw scores of the unit after.  LDS operands are read LA MFMAs ahead.
-  constexpr int NP = 4 * DB, NT = 2 * KC + NP, LA = 4;
-  constexpr int DL = 5, ST = 8 + DL;
-  u32x4 pp[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}, pd[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
-  u32x4 op[LA];
-  f32x16 dp;
-  auto rd = [&](int x, int half) {
-    if (x < KC) {
-      op[x % LA] = lds_rows(da[x / TL::PER] + half * HALF + TL::row_step(x));
-    } else if (x < KC + NP) {
-      const int y = x - KC, c = y / (2 * DB), db = y % (2 * DB) / 2;
-      const int o = (y & 1 ? 0 : TILE) + (half ^ 1) * HALF;
-      op[x % LA] = lds_turned(ta[db] + o + TL::turn_step(c, 0), ta[db] + o + TL::turn_step(c, 1));
-    } else if (x < NT) {
-      const int kc = x - KC - NP;
-      op[x % LA] = lds_rows(ra[kc / TL::PER] + (half ^ 1) * HALF + TL::row_step(kc));
+  // One unit of 32 query rows, the tile's half at byte offset `at` of its buffer.
+  constexpr int LA = 4;                                            // LDS operands ahead of their MFMA
+  auto unit = [&](int row0, int buf, int half, auto masked_tag) {
+    constexpr bool MASKED = decltype(masked_tag)::value;
+    const int at = buf * BUF + half * TL::HALF;
+    auto scalars = [&](int which, int x) {                         // rows 8 x + 4 g2 .. + 3
+      return lds_floats(sa + buf * BUF + half * 512 + which * 128 + 32 * x);
+    };
+    u32x4 op[LA], ov[2], ok[NKL ? NKL : 1];
+    f32x16 s{}, dp;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const f32x4 nd = scalars(2, x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dp[4 * x + i] = nd[i];
     }
-  };
-  auto step = [&](int x, f32x16& sn) {
-    if (x < KC) {
-      dp = mfma(op[x % LA], vf[x], dp);
-    } else if (x < KC + NP) {
-      const int y = x - KC, c = y / (2 * DB), db = y % (2 * DB) / 2;
-      if (y & 1) dka[db] = mfma(op[x % LA], pd[c], dka[db]);
-      else dva[db] = mfma(op[x % LA], pp[c], dva[db]);
-    } else {
-      sn = mfma(op[x % LA], kf[x - KC - NP], sn);
+    auto rd = [&](int x) {
+      const int kc = x >> 1;
+      if (x >= 2 * KC) return;
+      op[x % LA] = lds_rows(ra[kc / TL::PER] + at + (x & 1 ? TILE : 0) + TL::row_step(kc));
+      if (VLDS && (x & 1)) ov[kc & 1] = lds_rows(va + kc * 1024);
+      if (!(x & 1) && kc < NKL) ok[kc] = lds_rows(va + (KC + kc) * 1024);
+    };
+#pragma unroll
+    for (int x = 0; x < LA; ++x) rd(x);
+#pragma unroll
+    for (int x = 0; x < 2 * KC; ++x) {
+      if (x & 1) dp = mfma(op[x % LA], VLDS ? ov[(x >> 1) & 1] : vf[VLDS ? 0 : x >> 1], dp);
+      else s = mfma(op[x % LA], (x >> 1) < NKL ? ok[(x >> 1) % (NKL ? NKL : 1)] : kf[(x >> 1) - NKL], s);
+      rd(x + LA);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  };
-
-  // One unit, its raw scores in s; those of the next are left in sn.  MODE 0: every key precedes
-  // every row; 1: the diagonal; 2: no pair of the unit counts.
-  auto unit = [&](int row0, f32x16& s, f32x16& sn, auto half_tag, auto mode_tag) {
-    constexpr int H = decltype(half_tag)::value, MODE = decltype(mode_tag)::value;
-    sn = f32x16{};
-    Packer kp, kd;
-    if constexpr (MODE == 2) {
+    Packer pp, pd;
+    f32x4 nl[4], bt[4], kap[4];
+    bt[0] = scalars(1, 0);
+    constexpr int DL = 3;
+    unit_scores<DL, ADD, MASKED>(
+        g, s, dp, [&](int i) { return RowScalars{bt[i >> 2][i & 3], nl[i >> 2][i & 3], kap[i >> 2][i & 3]}; },
+        [&](int i, bool& valid, bool& diag) {
+          const int row = row0 + 8 * (i >> 2) + 4 * g2 + (i & 3);
+          valid = j <= row;
+          diag = j == row;
+        },
+        [&](int i, float p, float ds, float) {
+          pp.put(i, p);
+          pd.put(i, ds);
+        },
+        [&](int st) {        // the scalars of four rows are read a step before the first of them is due
+          if (st % 2 == 1 && st < 7) bt[(st + 1) / 2] = scalars(1, (st + 1) / 2);
+          if (st % 2 == 1 && st < 8) nl[st / 2] = scalars(0, st / 2);
+          if (st >= DL - 1 && (st - DL + 1) % 2 == 0 && st < DL + 7) kap[(st - DL + 1) / 2] = scalars(3, (st - DL + 1) / 2);
+        });
+    auto rt = [&](int x) {
+      const int c = x / (2 * DB), db = x % (2 * DB) / 2;
+      if (x >= 4 * DB) return;
+      const uint32_t o = ta[db] + at + (x & 1 ? 0 : TILE);
+      op[x % LA] = lds_turned(o + TL::turn_step(c, 0), o + TL::turn_step(c, 1));
+    };
 #pragma unroll
-      for (int x = KC; x < KC + LA; ++x) rd(x, H);
+    for (int x = 0; x < LA; ++x) rt(x);
 #pragma unroll
-      for (int x = KC; x < NT; ++x) {
-        step(x, sn);
-        rd(x + LA, H);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) kp.o[i] = kd.o[i] = u32x4{0, 0, 0, 0};
-    } else {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const f32x4 nd = scalars(2, H, x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dp[4 * x + i] = nd[i];
-      }
-#pragma unroll
-      for (int x = 0; x < LA; ++x) rd(x, H);
-      f32x4 nl[4], bt[4], kap[4];
-      bt[0] = scalars(1, H, 0);
-      unit_scores<DL, ADD, MODE == 1>(
-          g, s, dp,
-          [&](int i) {
-            return RowScalars{bt[i >> 2][i & 3], nl[i >> 2][i & 3], kap[i >> 2][i & 3]};
-          },
-          [&](int i, bool& valid, bool& diag) {
-            const int row = row0 + 8 * (i >> 2) + 4 * g2 + (i & 3);
-            valid = j <= row;
-            diag = j == row;
-          },
-          [&](int i, float p, float ds, float) {
-            kp.put(i, p);
-            kd.put(i, ds);
-          },
-          [&](int st) {
-            // the scalars of four rows are read a step before the first of them is due
-            if (st % 2 == 1 && st < 7) bt[(st + 1) / 2] = scalars(1, H, (st + 1) / 2);
-            if (st % 2 == 1 && st < 8) nl[st / 2] = scalars(0, H, st / 2);
-            if (st >= DL - 1 && (st - DL + 1) % 2 == 0 && st < DL + 7) kap[(st - DL + 1) / 2] = scalars(3, H, (st - DL + 1) / 2);
-#pragma unroll
-            for (int x = 0; x < NT; ++x)
-              if ((x < KC ? x * (DL - 1) / KC : DL - 1 + (x - KC) * (ST - DL + 1) / (NT - KC)) == st) {
-                step(x, sn);
-                rd(x + LA, H);
-              }
-          });
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      pp[i] = kp.o[i];
-      pd[i] = kd.o[i];
+    for (int x = 0; x < 4 * DB; ++x) {
+      const int c = x / (2 * DB), db = x % (2 * DB) / 2;
+      if (x & 1) dka[db] = mfma(op[x % LA], pd.o[c], dka[db]);
+      else dva[db] = mfma(op[x % LA], pp.o[c], dva[db]);
+      rt(x + LA);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  if (steps > 0) {
-    constexpr std::integral_constant<int, 0> c0{};
-    constexpr std::integral_constant<int, 1> c1{};
-    constexpr std::integral_constant<int, 2> c2{};
-    fetch(0);
-    if (steps > 1) fetch(1);
+  // At the start of a tile it has arrived (the barrier says so for every wavefront's part) and every
+  // wavefront is done with the other buffer.
+  int it = 0;
+  auto arrive = [&](int buf) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    f32x16 s0, s1{};
-    // (the products before the first unit are of zeros with tile 0's rows)
-#pragma unroll
-    for (int x = 0; x < KC; ++x) s1 = mfma(lds_rows(ra[x / TL::PER] + HALF + TL::row_step(x)), kf[x], s1);
-    // Tile `it` (buffer it % 3): its upper half beside the tile before, then its lower half beside the
-    // tile after.  In between tile it + 1 has arrived and the buffer of tile it - 1 is free.
-    int buf = 0, it = 0;
-    auto between = [&] {
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      if (it + 2 < steps) fetch(buf == 0 ? 2 : buf - 1);
-      const uint32_t on = buf == 2 ? -2u * BUF : (uint32_t)BUF, was = buf == 0 ? -2u * BUF : (uint32_t)BUF;
-      if (it > 0)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) ta[db] += was;
-      if (it + 1 < steps)
-#pragma unroll
-        for (int i = 0; i < TL::NR; ++i) ra[i] += on;
-    };
-    auto after = [&] {
-      const uint32_t on = buf == 2 ? -2u * BUF : (uint32_t)BUF;
-#pragma unroll
-      for (int i = 0; i < TL::NR; ++i) da[i] += on;
-      sa += on;
-      buf = buf == 2 ? 0 : buf + 1;
-      ++it;
-    };
+    if (++it < steps) fetch(buf ^ 1);
+  };
+  if (steps > 0) {
+    fetch(0);
+    constexpr std::integral_constant<bool, false> plain{};
+    constexpr std::integral_constant<bool, true> masked{};
     for (int hh = 0; hh < GH; ++hh) {
-#pragma unroll 1
-      for (int qb = nqb - 1; qb > 2 * kblk + 1; --qb) {
-        unit(qb * kGrT + 32, s1, s0, c1, c0);
-        between();
-        unit(qb * kGrT, s0, s1, c0, c0);
-        after();
-      }
-#pragma unroll 1
-      for (int qb = 2 * kblk + 1; qb >= 2 * kblk; --qb) {
-        if (2 * qb + 1 >= ku) unit(qb * kGrT + 32, s1, s0, c1, c1);
-        else unit(qb * kGrT + 32, s1, s0, c1, c2);
-        between();
-        if (2 * qb >= ku) unit(qb * kGrT, s0, s1, c0, c1);
-        else unit(qb * kGrT, s0, s1, c0, c2);
-        after();
-      }
-    }
-    // the last unit's products: turned rows of the last tile's lower half
+      int t = nt - 1;
+      for (; t >= t0 + kGrQ / TR; t -= 2) {
 #pragma unroll
-    for (int x = KC; x < KC + NP; ++x) {
-      rd(x, 1);
-      step(x, s0);
+        for (int buf = 0; buf < 2; ++buf) {
+          arrive(buf);
+#pragma unroll
+          for (int x = UT - 1; x >= 0; --x) unit((t - buf) * TR + 32 * x, buf, x, plain);
+        }
+      }
+      // the keys' own rows: a wavefront's units before its diagonal hold no pair
+#pragma unroll 1
+      for (; t >= t0; --t) {
+        const int buf = (t & 1) ^ 1;
+        arrive(buf);
+#pragma unroll 1
+        for (int x = UT - 1; x >= 0; --x)
+          if (UT * t + x >= ku) unit(t * TR + 32 * x, buf, x, masked);
+      }
     }
   }
 
@@ -709,7 +656,6 @@ hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, 
   a.T = pd.capacity_tokens;
   a.Tp = p.rows;
   a.nsplit = p.nsplit;
-  a.stat_step = (int64_t)pd.batch * pd.num_q_heads * p.rows;
   a.part_step = (int64_t)p.nsplit * pd.batch * pd.num_kv_heads * pd.capacity_tokens * pd.head_dim;
   a.beta = pd.beta;
   a.C = pd.additive ? pd.C : 0.f;

@@ -53,7 +53,7 @@ struct PrefillGradPtrs {
   const int32_t* seq_lens;
   void *dq, *dk, *dv;
   float* dtau;
-  float* stats;              // [4][batch num_q_heads][rows]
+  float* stats;              // [batch num_q_heads][rows / 32][4][32]
   float* part;               // [2][nsplit][batch num_kv_heads][capacity_tokens][head_dim], nsplit > 1
 };
 size_t prefill_grad_bytes(const eta_prefill_desc_t& pd, const GradPlan& p, PrefillGradPtrs* carve, void* base);
