@@ -571,8 +571,8 @@ typedef enum {
   ETA_KERNEL_QK_ROPE = 11,
   ETA_KERNEL_QK_ROPE_GRAD = 12,
   ETA_KERNEL_QK_WEIGHT_GRAD = 13,
-  ETA_KERNEL_PREFILL_GRAD_Q = 14,
-  ETA_KERNEL_PREFILL_GRAD_KV = 15,
+  ETA_KERNEL_PREFILL_GRAD_ROWS = 14,
+  ETA_KERNEL_PREFILL_GRAD = 15,
   ETA_KERNEL_PREFILL_GRAD_JOIN = 16,
   ETA_KERNEL_ALL_KINDS = 17
 } eta_kernel_kind_t;

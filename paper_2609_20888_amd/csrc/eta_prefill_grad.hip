@@ -7,6 +7,7 @@
 
 #include <type_traits>
 
+#include "eta_lanes.h"
 #include "eta_tile.h"
 #include "eta_train.h"
 
@@ -20,13 +21,15 @@ namespace {
 //   dq_i = sum_j dS k_j / sqrt(d),  dk_j = sum_i dS q_i / sqrt(d),  dv_j = sum_i P dO_i;
 // on the diagonal S~ = S, so dS = dS~ + sg' beta dR_i.
 //
-// Two passes, so that every sum has one owner and a fixed order: grad_q_kernel owns 128 query
-// rows and walks over the keys (dq, dtau), grad_kv_kernel owns 128 keys and walks over the
-// query rows and the heads of its group (dk, dv).  Each forms S and dO.v anew: seven products
-// for the five that one pass would need, whose dq would have to be added up in memory from
-// every block of keys (512 bytes a row for each 128 keys, in an order that changes).
-// What bounds them: vector-ALU issue, as in the forward (three transcendentals and about
-// twelve other instructions for a score in either pass).
+// Every sum has one owner and a fixed order: a workgroup owns either 128 query rows and walks over
+// the keys (dq, dtau), or 128 keys and walks over the query rows and the heads of its group (dk,
+// dv).  Each kind forms S and dO.v anew: seven products for the five that one walk would need, whose
+// dq would have to be added up in memory from every block of keys (512 bytes a row for each 128
+// keys, in an order that changes).  Both kinds run in one launch, the longest walks first, so that
+// short ones fill the compute units beside the last long ones; the row scalars that both read (D
+// among them) come from a small launch before.
+// What bounds it: vector-ALU issue, as in the forward (three transcendentals and about a dozen
+// other instructions for a score of either kind).
 
 constexpr int kGrQ = 128;    // rows (queries or keys) a workgroup owns, 32 per wavefront
 constexpr int kGrT = 64;     // rows of a streamed tile
@@ -40,7 +43,7 @@ struct GradArgs {
   float* stats;              // [B Hq][Tp / 32][4][32]: -L', beta tau' + log2 is2, -D, beta dR
   float* part;               // [2][nsplit][B Hkv][T][d] partial dk, dv (nsplit > 1)
   int64_t part_step;         // nsplit B Hkv T d
-  int Hq, Hkv, T, Tp, nsplit;
+  int B, Hq, Hkv, T, Tp, nsplit;
   float beta, C;
 };
 
@@ -135,20 +138,31 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
   }
 }
 
-// The work of workgroup `wg` of nb blocks and NH (head, sequence) pairs: blocks in order of
-// `blk` (the caller puts the longest first), and with a multiple of eight heads neighbouring
-// heads on one XCD (workgroups are dealt to the eight XCDs round robin).
-__device__ __forceinline__ void grad_work(uint32_t wg, uint32_t H, uint32_t NH, int& blk, int& h, int& b) {
-  blk = (int)(wg / NH);
-  const uint32_t hi = wg % NH;
+// The work of a workgroup: blocks of 128 rows by length of their walk, the longest first, and at
+// each length all (key head, head split, sequence) then all (query head, sequence).  With a multiple of
+// eight heads neighbouring heads, which share K and V, are on one XCD (workgroups are dealt to the
+// eight XCDs round robin).
+struct GradWork {
+  bool keys;
+  int blk, h, b;             // h: query head, or key head * nsplit + split
+};
+__device__ __forceinline__ GradWork grad_work(const GradArgs& a, uint32_t wg, int blocks) {
+  const uint32_t nk = (uint32_t)(a.Hkv * a.nsplit * a.B), nq = (uint32_t)(a.Hq * a.B), rank = wg / (nk + nq);
+  uint32_t i = wg % (nk + nq);
+  GradWork x;
+  x.keys = i < nk;
+  if (!x.keys) i -= nk;
+  x.blk = x.keys ? (int)rank : blocks - 1 - (int)rank;
+  const uint32_t H = (uint32_t)(x.keys ? a.Hkv * a.nsplit : a.Hq);
   if ((H & 7) == 0) {
-    const uint32_t hpx = H / 8, r = hi / 8;
-    h = (int)((hi % 8) * hpx + r % hpx);
-    b = (int)(r / hpx);
+    const uint32_t hpx = H / 8, r = i / 8;
+    x.h = (int)((i % 8) * hpx + r % hpx);
+    x.b = (int)(r / hpx);
   } else {
-    h = (int)(hi % H);
-    b = (int)(hi / H);
+    x.h = (int)(i % H);
+    x.b = (int)(i / H);
   }
+  return x;
 }
 
 // A tile of rows of D bf16 in LDS: groups of 1 KiB (what a wavefront's direct load writes), 16 bytes
@@ -242,27 +256,50 @@ struct Packer {
   }
 };
 
-__device__ __forceinline__ float dot_bf16(const u32x4& a, const u32x4& b, float s) {
+// The row scalars (GradArgs::stats): D_i = dO_i.O_i - dL_i, the lanes of a row 16 bytes each.  Rows at or past
+// the sequence's end, up to a whole block, get P = 0 and no gradient.  Bound by reading O and dO.
+template <int D>
+__global__ __launch_bounds__(256) void grad_rows_kernel(GradArgs a) {
+  constexpr int LPR = D / 8, RPW = 256 / LPR;
+  const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / LPR;      // (Tp is a multiple of RPW)
+  const int64_t head = row / a.Tp;
+  const int t = (int)(row - head * a.Tp), c = threadIdx.x % LPR;
+  const bool in = t < (int)clamp_len(a.seq_lens, (int)(head / a.Hq), a.T);
+  const int64_t at = head * a.T + (in ? t : 0);
+  float s = 0.f;
+  if (in) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(a.dout + at * D + 8 * c), y = *reinterpret_cast<const u32x4*>(a.out + at * D + 8 * c);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    s = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16), s);
-    s = fmaf(__uint_as_float(a[i] & 0xffff0000u), __uint_as_float(b[i] & 0xffff0000u), s);
+    for (int i = 0; i < 4; ++i) {
+      s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+      s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+    }
   }
-  return s;
+  s = lanes_sum<LPR>(s);
+  if (c < 4) {
+    float v = c == 0 ? kNegInf : 0.f;
+    if (in) {
+      if (c == 0) v = -a.L[at] * kLog2e;
+      if (c == 1) v = a.beta * kLog2e * a.tau[at];
+      if (c == 2) v = a.dL ? a.dL[at] - s : -s;
+      if (c == 3) v = a.dR ? a.beta * a.dR[at] : 0.f;
+    }
+    const float s2 = kLog2e / sqrtf((float)D);
+    if (c == 1) v -= log2f(s2);
+    a.stats[(head * a.Tp + (t & ~31)) * 4 + 32 * c + (t & 31)] = v;
+  }
 }
 
-// dq, dtau of 128 query rows, and the row scalars that grad_kv_kernel reads.  As in the forward
-// each lane owns a query row: S^T = K Q^T and dP^T = V dO^T with A from LDS, dq^T += K^T dS^T with
-// the lane's own dS (bf16) as B and K^T from transpose reads.
+// dq, dtau of 128 query rows.  As in the forward each lane owns a query row: S^T = K Q^T and dP^T =
+// V dO^T - D with A from LDS, dq^T += K^T dS^T with the lane's own dS (bf16) as B and K^T from transpose
+// reads.
+template <int D>
+constexpr int kGradQLds = 4 * Tile<D>::BYTES;
 template <int D, bool ADD>
-__global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
+__device__ __forceinline__ void grad_q(const GradArgs& a, char* lds, int qblk, int h, int b) {
   constexpr int KC = D / 16, DB = D / 32;
   using TL = Tile<D>;
-  __shared__ __attribute__((aligned(16))) char lds[2][2 * TL::BYTES];        // K, V
-  const uint32_t nqb = gridDim.x, NH = gridDim.y * gridDim.z;
-  int blk, h, b;
-  grad_work(blockIdx.x + nqb * (blockIdx.y + gridDim.y * blockIdx.z), (uint32_t)a.Hq, NH, blk, h, b);
-  const int qblk = (int)nqb - 1 - blk;
+  constexpr int BUF = 2 * TL::BYTES;                                // K, V; two buffers
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, g2 = lane >> 5;
   const int Tb = (int)clamp_len(a.seq_lens, b, a.T);
@@ -272,38 +309,23 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
 
   const int wrow0 = qblk * kGrQ + 32 * w, t = wrow0 + r32, tq = min(t, max(Tb, 1) - 1);
   u32x4 qb[KC], dob[KC];
-  float dsum = 0.f;
 #pragma unroll
   for (int kc = 0; kc < KC; ++kc) {
     const int64_t at = (qrow0 + tq) * D + 16 * kc + 8 * g2;
     qb[kc] = *reinterpret_cast<const u32x4*>(a.q + at);
     dob[kc] = *reinterpret_cast<const u32x4*>(a.dout + at);
-    dsum = dot_bf16(dob[kc], *reinterpret_cast<const u32x4*>(a.out + at), dsum);
   }
-  // row scalars; rows at or past the sequence's end take P = 0 and no gradient
   const bool in = t < Tb;
-  float nl = kNegInf, bt = g.lis2, nd = 0.f, kap = 0.f;
-  if (in) {
-    nl = -a.L[qrow0 + t] * kLog2e;
-    bt = fmaf(a.beta * kLog2e, a.tau[qrow0 + t], g.lis2);
-    nd = -row2_sum(dsum);
-    if (a.dL) nd += a.dL[qrow0 + t];
-    if (a.dR) kap = a.beta * a.dR[qrow0 + t];
-  }
-  if (g2 == 0) {
-    float* st = a.stats + (head * a.Tp + wrow0) * 4 + r32;
-    st[0] = nl;
-    st[32] = bt;
-    st[64] = nd;
-    st[96] = kap;
-  }
+  const float* st = a.stats + (head * a.Tp + wrow0) * 4 + r32;
+  const RowScalars rs{st[32], st[0], st[96]};
+  const float nd = st[64];
 
   const TileLoad<D> load(tid);
   uint32_t ra[TL::NR], ta[DB];
 #pragma unroll
-  for (int i = 0; i < TL::NR; ++i) ra[i] = lds_address(lds[0]) + TL::row_base(lane, i);
+  for (int i = 0; i < TL::NR; ++i) ra[i] = lds_address(lds) + TL::row_base(lane, i);
 #pragma unroll
-  for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds[0]) + TL::turn_base(lane, db);
+  for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds) + TL::turn_base(lane, db);
   const uint16_t *kh = a.k + kvoff, *vh = a.v + kvoff;
   const int last_row = min(qblk * kGrQ + kGrQ, Tb) - 1;
   const int nkb = last_row >= qblk * kGrQ ? last_row / kGrT + 1 : 0;
@@ -312,7 +334,6 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = f32x16{};
   float nsum = 0.f;
-  const RowScalars rs{bt, nl, kap};
 
   // One unit of 32 keys: the score products, the vector work, the product into dq.  Nothing of a
   // wavefront overlaps with its own vector work; the other wavefront of the SIMD's does.
@@ -372,13 +393,13 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (kb + 1 < nkb) {
-      load(kh, lds[buf ^ 1], w, kb + 1, Tb);
-      load(vh, lds[buf ^ 1] + TL::BYTES, w, kb + 1, Tb);
+      load(kh, lds + (buf ^ 1) * BUF, w, kb + 1, Tb);
+      load(vh, lds + (buf ^ 1) * BUF + TL::BYTES, w, kb + 1, Tb);
     }
   };
   if (nkb > 0) {
-    load(kh, lds[0], w, 0, Tb);
-    load(vh, lds[0] + TL::BYTES, w, 0, Tb);
+    load(kh, lds, w, 0, Tb);
+    load(vh, lds + TL::BYTES, w, 0, Tb);
     constexpr std::integral_constant<bool, false> plain{};
     constexpr std::integral_constant<bool, true> masked{};
     // the blocks before the workgroup's rows (an even number of them) need no mask
@@ -388,7 +409,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
         arrive(kb + buf, buf);
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-          unit(2 * (kb + buf) + x, buf * 2 * TL::BYTES + x * TL::HALF, plain);
+          unit(2 * (kb + buf) + x, buf * BUF + x * TL::HALF, plain);
       }
     }
 #pragma unroll 1
@@ -396,7 +417,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
       arrive(kb, kb & 1);
 #pragma unroll 1
       for (int u = 2 * kb; u < min(2 * kb + 2, nu); ++u)
-        unit(u, (kb & 1) * 2 * TL::BYTES + (u & 1) * TL::HALF, masked);
+        unit(u, (kb & 1) * BUF + (u & 1) * TL::HALF, masked);
     }
   }
 
@@ -424,18 +445,22 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs a) {
 // wavefronts fit a SIMD and the matrix work of one runs beside the vector work of the other.
 // (With V in registers too only one fits: 3.2K cycles a unit with all its matrix work threaded
 // through the vector work, a quarter of them waits.)
+template <int D>
+struct KeyWalk {
+  static constexpr bool VLDS = D == 128;
+  static constexpr int TR = D == 128 ? 32 : 64, UT = TR / 32;      // rows and units of a tile
+  static constexpr int NKL = VLDS ? 2 : 0;                         // K operands kept in LDS
+  static constexpr int TILE = UT * Tile<D>::HALF, BUF = 2 * TILE + 4 * TR * 4;
+  static constexpr int VB = VLDS ? 4 * (D / 16 + NKL) * 1024 : 0;
+  static constexpr int LDS = VB + 2 * BUF;                         // V (and K operands), then twice: Q, dO, row scalars
+};
 template <int D, bool ADD>
-__global__ __launch_bounds__(256, 2) void grad_kv_kernel(GradArgs a) {
+__device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, int hs, int b) {
   constexpr int KC = D / 16, DB = D / 32;
-  constexpr bool VLDS = D == 128;
-  constexpr int TR = D == 128 ? 32 : 64, UT = TR / 32;             // rows and units of a tile
   using TL = Tile<D>;
-  constexpr int TILE = UT * TL::HALF, BUF = 2 * TILE + 4 * TR * 4, NKL = VLDS ? 2 : 0;
-  constexpr int VB = VLDS ? 4 * (KC + NKL) * 1024 : 0;             // bytes
-  __shared__ __attribute__((aligned(16))) char lds[VB + 2 * BUF];  // V (and two operands of K), then twice: Q, dO, row scalars
-  const uint32_t NH = gridDim.y * gridDim.z;
-  int kblk, hs, b;
-  grad_work(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), (uint32_t)gridDim.y, NH, kblk, hs, b);
+  using KW = KeyWalk<D>;
+  constexpr bool VLDS = KW::VLDS;
+  constexpr int TR = KW::TR, UT = KW::UT, NKL = KW::NKL, TILE = KW::TILE, BUF = KW::BUF, VB = KW::VB;
   const int kvh = hs / a.nsplit, split = hs % a.nsplit;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, g2 = lane >> 5;
@@ -593,7 +618,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(GradArgs a) {
 
   if (j < a.T) {
     if (a.nsplit > 1) {
-      float* o = a.part + (((int64_t)split * gridDim.z * a.Hkv + (int64_t)b * a.Hkv + kvh) * a.T + j) * D + 4 * g2;
+      float* o = a.part + (((int64_t)(split * a.B + b) * a.Hkv + kvh) * a.T + j) * D + 4 * g2;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -616,6 +641,14 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(GradArgs a) {
         }
     }
   }
+}
+
+template <int D, bool ADD>
+__global__ __launch_bounds__(256, 2) void grad_kernel(GradArgs a, int blocks) {
+  __shared__ __attribute__((aligned(16))) char lds[kGradQLds<D> > KeyWalk<D>::LDS ? kGradQLds<D> : KeyWalk<D>::LDS];
+  const GradWork x = grad_work(a, blockIdx.x, blocks);
+  if (x.keys) grad_kv<D, ADD>(a, lds, x.blk, x.h, x.b);
+  else grad_q<D, ADD>(a, lds, x.blk, x.h, x.b);
 }
 
 // dk (blockIdx.y 0) or dv (1) from the head splits' partials, added in order; four values a thread.
@@ -651,6 +684,7 @@ hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, 
   a.dtau = x.dtau;
   a.stats = x.stats;
   a.part = x.part;
+  a.B = pd.batch;
   a.Hq = pd.num_q_heads;
   a.Hkv = pd.num_kv_heads;
   a.T = pd.capacity_tokens;
@@ -659,24 +693,20 @@ hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, 
   a.part_step = (int64_t)p.nsplit * pd.batch * pd.num_kv_heads * pd.capacity_tokens * pd.head_dim;
   a.beta = pd.beta;
   a.C = pd.additive ? pd.C : 0.f;
-  const dim3 gq(p.blocks, pd.num_q_heads, pd.batch), gk(p.blocks, pd.num_kv_heads * p.nsplit, pd.batch);
-  hipError_t e = with_hook(hook, ETA_KERNEL_PREFILL_GRAD_Q, stream, [&] {
-    if (pd.additive) {
-      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_q_kernel<64, true>), gq, dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((grad_q_kernel<128, true>), gq, dim3(256), 0, stream, a);
-    } else {
-      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_q_kernel<64, false>), gq, dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((grad_q_kernel<128, false>), gq, dim3(256), 0, stream, a);
-    }
+  hipError_t e = with_hook(hook, ETA_KERNEL_PREFILL_GRAD_ROWS, stream, [&] {
+    const int64_t rows = (int64_t)pd.batch * pd.num_q_heads * p.rows;
+    if (pd.head_dim == 64) hipLaunchKernelGGL((grad_rows_kernel<64>), dim3((uint32_t)(rows / 32)), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((grad_rows_kernel<128>), dim3((uint32_t)(rows / 16)), dim3(256), 0, stream, a);
   });
   if (e != hipSuccess) return e;
-  e = with_hook(hook, ETA_KERNEL_PREFILL_GRAD_KV, stream, [&] {
+  const dim3 grid((uint32_t)((int64_t)p.blocks * pd.batch * (pd.num_q_heads + pd.num_kv_heads * p.nsplit)));
+  e = with_hook(hook, ETA_KERNEL_PREFILL_GRAD, stream, [&] {
     if (pd.additive) {
-      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_kv_kernel<64, true>), gk, dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((grad_kv_kernel<128, true>), gk, dim3(256), 0, stream, a);
+      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_kernel<64, true>), grid, dim3(256), 0, stream, a, p.blocks);
+      else hipLaunchKernelGGL((grad_kernel<128, true>), grid, dim3(256), 0, stream, a, p.blocks);
     } else {
-      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_kv_kernel<64, false>), gk, dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((grad_kv_kernel<128, false>), gk, dim3(256), 0, stream, a);
+      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_kernel<64, false>), grid, dim3(256), 0, stream, a, p.blocks);
+      else hipLaunchKernelGGL((grad_kernel<128, false>), grid, dim3(256), 0, stream, a, p.blocks);
     }
   });
   if (e != hipSuccess || p.nsplit == 1) return e;

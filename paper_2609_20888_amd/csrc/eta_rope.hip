@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "eta_device.h"
+#include "eta_lanes.h"
 #include "eta_train.h"
 
 namespace eta {
@@ -54,24 +55,6 @@ struct Piece<float> {
                       __float_as_uint(x[3]));
   }
 };
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
-}
-// sum over the N = 8, 16 or 32 lanes of a row, the same in each of them
-template <int N>
-__device__ __forceinline__ float row_sum(float x) {
-  x = dpp_add<0xB1>(x);                         // quad_perm [1,0,3,2]
-  x = dpp_add<0x4E>(x);                         // quad_perm [2,3,0,1]
-  x = dpp_add<0x141>(x);                        // row_half_mirror
-  if constexpr (N >= 16) x = dpp_add<0x140>(x); // row_mirror
-  if constexpr (N >= 32) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  }
-  return x;
-}
 
 struct RopeArgs {
   const char *q, *k, *v;          // projections [B][Tn][H][d] (byte strides below)
@@ -233,7 +216,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
-        rs = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + a.eps);
+        rs = rsqrtf(lanes_sum<LPR>(ss) * (1.0f / D) + a.eps);
       }
       if (a.interleaved) {
 #pragma unroll
@@ -324,7 +307,7 @@ __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
             Piece<T>::unpack(rx[u], x);
 #pragma unroll
             for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
-            const float rs = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + a.eps);
+            const float rs = rsqrtf(lanes_sum<LPR>(ss) * (1.0f / D) + a.eps);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
               x[e] *= rs;
@@ -332,7 +315,7 @@ __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
               if (row) dw[e] += p;
               sg = fmaf(p, w[e], sg);
             }
-            sg = row_sum<LPR>(sg) * (1.0f / D);
+            sg = lanes_sum<LPR>(sg) * (1.0f / D);
 #pragma unroll
             for (int e = 0; e < E; ++e) g[e] = rs * fmaf(-x[e], sg, g[e] * w[e]);
           }

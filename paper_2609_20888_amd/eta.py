@@ -21,7 +21,7 @@ ETA_OK, ETA_ERR_INVALID_ARG, ETA_ERR_UNSUPPORTED, ETA_ERR_WORKSPACE, ETA_ERR_HIP
 ETA_DT_F32, ETA_DT_BF16, ETA_DT_F16, ETA_DT_FP8 = 0, 1, 2, 3
 KERNEL_KINDS = ("summaries", "predict", "screen", "split_decode", "combine", "dense_split",
                 "dense_combine", "bounds", "calib_accumulate", "calib_solve", "prefill",
-                "qk_rope", "qk_rope_grad", "qk_weight_grad", "prefill_grad_q", "prefill_grad_kv",
+                "qk_rope", "qk_rope_grad", "qk_weight_grad", "prefill_grad_rows", "prefill_grad",
                 "prefill_grad_join")
 
 _vp = ctypes.c_void_p
