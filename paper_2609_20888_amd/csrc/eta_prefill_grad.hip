@@ -79,8 +79,8 @@ struct RowScalars {
 // The vector work of a unit: 16 scores of a lane, raw products in s and dO.v - D in dp, two
 // scores a step, the four stages of a score one step apart so that no step waits for its own
 // transcendentals; the last stage, the first to read dp, DL steps after the first.  row(j) gives score j's scalars, mask(j, valid, diag) its place (MASKED),
-// done(j, p, ds, n) takes P, s2 dS and s2 sg' m; beside(step) is the matrix work of a step.
-template <int DL, bool ADD, bool MASKED, typename Row, typename Mask, typename Done, typename Beside>
+// done(j, p, ds, n) takes P, s2 dS and s2 sg' m (the last with TAU only); beside(step) is the matrix work of a step.
+template <int DL, bool ADD, bool MASKED, bool TAU, typename Row, typename Mask, typename Done, typename Beside>
 __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, const f32x16& dp, Row row, Mask mask,
                                             Done done, Beside beside) {
   float e[16], u[16], w[16], p[16];       // (a few of each are alive at a time)
@@ -101,14 +101,16 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
           m = valid ? m : 0.f;
         }
         const float n = w[o] * m;
-        done(j, p[o], fmaf(d, lin, n), n);
+        if constexpr (TAU || ADD || MASKED) done(j, p[o], fmaf(d, lin, n), n);
+        else done(j, p[o], u[o] * fmaf(w[o], m, d), 0.f);
       }
     }
     if (st >= 2 && st < 10) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int j = 2 * (st - 2) + i, o = j;
-        w[o] = u[o] * eta_mul_legacy(u[o], e[o]);
+        w[o] = eta_mul_legacy(u[o], e[o]);              // 1 - sg
+        if constexpr (TAU || ADD || MASKED) w[o] *= u[o];
         const float nl = row(j).nl;
         float y = ADD ? fmaf(g.C2is, u[o], fmaf(s[j], g.s2, nl - g.C2)) : fmaf(s[j], u[o], nl);
         if constexpr (MASKED) {
@@ -359,7 +361,7 @@ __device__ __forceinline__ void grad_q(const GradArgs& a, char* lds, int qblk, i
     }
     Packer pk;
     float un = 0.f;
-    unit_scores<3, ADD, MASKED>(
+    unit_scores<3, ADD, MASKED, true>(
         g, s, dp, [&](int) { return rs; },
         [&](int i, bool& valid, bool& diag) {
           const int j = u * 32 + 8 * (i >> 2) + 4 * g2 + (i & 3);
@@ -548,7 +550,7 @@ __device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, 
     f32x4 nl[4], bt[4], kap[4];
     bt[0] = scalars(1, 0);
     constexpr int DL = 3;
-    unit_scores<DL, ADD, MASKED>(
+    unit_scores<DL, ADD, MASKED, false>(
         g, s, dp, [&](int i) { return RowScalars{bt[i >> 2][i & 3], nl[i >> 2][i & 3], kap[i >> 2][i & 3]}; },
         [&](int i, bool& valid, bool& diag) {
           const int row = row0 + 8 * (i >> 2) + 4 * g2 + (i & 3);

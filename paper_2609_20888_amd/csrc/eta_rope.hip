@@ -23,6 +23,21 @@ namespace {
 // lanes of a row keep one token and walk over heads, so that sines, cosines and weights
 // stay in registers (a sine costs as much vector work as the rest of a row's value).
 
+// 16 bytes of a row, read once: with the non-temporal hint (16K tokens, 32/8 heads, d = 128, bf16,
+// backward: 125 -> 108 us; 4 x 2000, 32/4, d = 64, fp32: 46.5 -> 42.6 us).  The forward writes with it
+// too (STREAM) where the call's bytes pass what the last-level cache holds beside other work: 246 MB
+// 56 -> 52 us, 403 MB 88 -> 81 us; at 202 MB the two are equal, and below that what is written is
+// best left in the cache for its reader (fp32, 147 MB: 28 us, with the hint 30).
+typedef uint32_t u32x4n __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 get16(const char* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(p)));
+}
+template <bool STREAM>
+__device__ __forceinline__ void put16(char* p, const uint4& x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4n, x), reinterpret_cast<u32x4n*>(p));
+  else *reinterpret_cast<uint4*>(p) = x;
+}
+
 template <typename T>
 struct Piece;                     // 16 bytes of a row
 template <>
@@ -157,7 +172,7 @@ __device__ __forceinline__ Share share_of(const RopeArgs& a, int y) {
 
 constexpr int kRopeAhead = 4;     // rows of a lane in flight
 
-template <typename T, int D>
+template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   constexpr int E = Piece<T>::E, LPR = D / E, TPW = 256 / LPR;
   constexpr int64_t ROW = D * sizeof(T);
@@ -184,10 +199,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       uint4 r[kRopeAhead];
 #pragma unroll
       for (int u = 0; u < kRopeAhead; ++u)
-        r[u] = *reinterpret_cast<const uint4*>(in + min(h + u, sh.h1 - 1) * ROW);
+        r[u] = get16(in + min(h + u, sh.h1 - 1) * ROW);
 #pragma unroll
       for (int u = 0; u < kRopeAhead; ++u)
-        if (live && h + u < sh.h1) *reinterpret_cast<uint4*>(out + (h + u) * step) = r[u];
+        if (live && h + u < sh.h1) put16<STREAM>(out + (h + u) * step, r[u]);
     }
     return;
   }
@@ -206,7 +221,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     uint4 r[kRopeAhead];
 #pragma unroll
     for (int u = 0; u < kRopeAhead; ++u)
-      r[u] = *reinterpret_cast<const uint4*>(in + min(h + u, sh.h1 - 1) * ROW);
+      r[u] = get16(in + min(h + u, sh.h1 - 1) * ROW);
 #pragma unroll
     for (int u = 0; u < kRopeAhead; ++u) {
       float x[E], o[E];
@@ -229,7 +244,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         const float n = x[e] * rs;
         x[e] = turn.rotated ? fmaf(o[e] * rs, wo[e], n * w[e]) : n * w[e];
       }
-      if (live && h + u < sh.h1) *reinterpret_cast<uint4*>(out + (h + u) * step) = Piece<T>::pack(x);
+      if (live && h + u < sh.h1) put16<STREAM>(out + (h + u) * step, Piece<T>::pack(x));
     }
   }
 }
@@ -283,8 +298,8 @@ __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
 #pragma unroll
       for (int u = 0; u < kRopeAhead; ++u) {
         const int hh = min(h + u, sh.h1 - 1);
-        rg[u] = *reinterpret_cast<const uint4*>(g_in + hh * step);
-        if (wt) rx[u] = *reinterpret_cast<const uint4*>(x_in + hh * ROW);
+        rg[u] = get16(g_in + hh * step);
+        if (wt) rx[u] = get16(x_in + hh * ROW);
       }
 #pragma unroll
       for (int u = 0; u < kRopeAhead; ++u) {
@@ -322,7 +337,7 @@ __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
           res = Piece<T>::pack(g);
         }
         if (!live) res = make_uint4(0, 0, 0, 0);
-        if (in_range && h + u < sh.h1) *reinterpret_cast<uint4*>(out + (h + u) * ROW) = res;
+        if (in_range && h + u < sh.h1) put16<false>(out + (h + u) * ROW, res);
       }
     }
   }
@@ -339,26 +354,35 @@ __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
   }
 }
 
-// Sums of the rows of partials: one workgroup per 16 columns of q's or k's weight.
-// Thread (r, c) adds rows r, r + 16, ... of its column; the 16 sums are added in order.
-__global__ __launch_bounds__(256) void rope_weight_kernel(const float* part, int rows_q, int rows_k,
-                                                          int D, float* dqw, float* dkw) {
-  __shared__ float s[16][17];
+// Sums of the rows of partials: one workgroup per 16 columns of q's or k's weight.  Thread (r, c) adds
+// rows r, r + 64, ... of its column, sixteen loads at once (they, not the adds, are the time), and the
+// 64 sums are added in order.
+__global__ __launch_bounds__(1024) void rope_weight_kernel(const float* part, int rows_q, int rows_k,
+                                                           int D, float* dqw, float* dkw) {
+  static_assert(kRopePartials <= 64 * 16, "one batch of loads");
+  __shared__ float s[64][17];
   const int r = threadIdx.x / 16, c = threadIdx.x % 16;
   const bool key = blockIdx.y == 1;
   float* out = key ? dkw : dqw;
   if (out == nullptr) return;
   const float* p = part + (key ? (int64_t)rows_q * D : 0) + blockIdx.x * 16 + c;
   const int rows = key ? rows_k : rows_q;
-  float x = 0.f;
-  for (int i = r; i < rows; i += 16) x += p[(int64_t)i * D];
-  s[r][c] = x;
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int row = r + 64 * i;
+    x[i] = row < rows ? p[(int64_t)row * D] : 0.f;
+  }
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t += x[i];
+  s[r][c] = t;
   __syncthreads();
   if (r == 0) {
-    x = 0.f;
+    t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x += s[i][c];
-    out[blockIdx.x * 16 + c] = x;
+    for (int i = 0; i < 64; ++i) t += s[i][c];
+    out[blockIdx.x * 16 + c] = t;
   }
 }
 
@@ -401,14 +425,17 @@ RopeArgs rope_args(const eta_rope_desc_t& rd, const RopePlan& p, const float* qw
   return a;
 }
 
-template <typename F32D64, typename F32D128, typename H16D64, typename H16D128>
-void by_type(const eta_rope_desc_t& rd, F32D64 f64, F32D128 f128, H16D64 h64, H16D128 h128) {
-  if (rd.dtype == ETA_DT_F32) {
-    if (rd.head_dim == 64) f64(); else f128();
-  } else {
-    if (rd.head_dim == 64) h64(); else h128();
-  }
-}
+// Launches a kernel for the descriptor's type and head dimension (further template arguments after these).
+#define ETA_ROPE_LAUNCH(kernel, ...)                                                                                    \
+  do {                                                                                                                  \
+    if (rd.dtype == ETA_DT_F32) {                                                                                       \
+      if (rd.head_dim == 64) hipLaunchKernelGGL((kernel<float, 64 __VA_ARGS__>), grid, dim3(256), 0, stream, a);        \
+      else hipLaunchKernelGGL((kernel<float, 128 __VA_ARGS__>), grid, dim3(256), 0, stream, a);                         \
+    } else {                                                                                                            \
+      if (rd.head_dim == 64) hipLaunchKernelGGL((kernel<uint16_t, 64 __VA_ARGS__>), grid, dim3(256), 0, stream, a);     \
+      else hipLaunchKernelGGL((kernel<uint16_t, 128 __VA_ARGS__>), grid, dim3(256), 0, stream, a);                      \
+    }                                                                                                                   \
+  } while (0)
 
 }  // namespace
 
@@ -425,10 +452,8 @@ hipError_t launch_rope(const eta_rope_desc_t& rd, const RopePlan& p, const void*
   a.v_out = (char*)v_cache;
   const dim3 grid(p.tiles, p.nq + p.nk + p.nv);
   return with_hook(hook, ETA_KERNEL_QK_ROPE, stream, [&] {
-    by_type(rd, [&] { hipLaunchKernelGGL((rope_kernel<float, 64>), grid, dim3(256), 0, stream, a); },
-            [&] { hipLaunchKernelGGL((rope_kernel<float, 128>), grid, dim3(256), 0, stream, a); },
-            [&] { hipLaunchKernelGGL((rope_kernel<uint16_t, 64>), grid, dim3(256), 0, stream, a); },
-            [&] { hipLaunchKernelGGL((rope_kernel<uint16_t, 128>), grid, dim3(256), 0, stream, a); });
+    if (p.stream) ETA_ROPE_LAUNCH(rope_kernel, , true);
+    else ETA_ROPE_LAUNCH(rope_kernel, , false);
   });
 }
 
@@ -450,14 +475,11 @@ hipError_t launch_rope_grad(const eta_rope_desc_t& rd, const RopePlan& p, const 
   a.part = part;
   const dim3 grid(p.steps, p.nq + p.nk + p.nv);
   hipError_t e = with_hook(hook, ETA_KERNEL_QK_ROPE_GRAD, stream, [&] {
-    by_type(rd, [&] { hipLaunchKernelGGL((rope_grad_kernel<float, 64>), grid, dim3(256), 0, stream, a); },
-            [&] { hipLaunchKernelGGL((rope_grad_kernel<float, 128>), grid, dim3(256), 0, stream, a); },
-            [&] { hipLaunchKernelGGL((rope_grad_kernel<uint16_t, 64>), grid, dim3(256), 0, stream, a); },
-            [&] { hipLaunchKernelGGL((rope_grad_kernel<uint16_t, 128>), grid, dim3(256), 0, stream, a); });
+    ETA_ROPE_LAUNCH(rope_grad_kernel);
   });
   if (e != hipSuccess || (!qw && !kw)) return e;
   return with_hook(hook, ETA_KERNEL_QK_WEIGHT_GRAD, stream, [&] {
-    hipLaunchKernelGGL(rope_weight_kernel, dim3(rd.head_dim / 16, 2), dim3(256), 0, stream, part,
+    hipLaunchKernelGGL(rope_weight_kernel, dim3(rd.head_dim / 16, 2), dim3(1024), 0, stream, part,
                        p.nq * p.steps, p.nk * p.steps, rd.head_dim, qw ? dqw : nullptr, kw ? dkw : nullptr);
   });
 }

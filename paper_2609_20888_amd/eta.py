@@ -562,6 +562,29 @@ def gated_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: torch.
 
 
 # ---------------------------------------------------------------- around the prefill
+#
+# These calls are short (a decode step's rotation takes a few microseconds on the GPU), so what
+# the host does for one counts.  The checks of a call's tensors, its descriptor and its workspace
+# size depend on their shapes, strides, types and devices alone and are made once for each
+# combination of them.
+
+_PLANS: dict = {}
+_PLANS_MOST = 1024
+
+
+def _form(t: Optional[torch.Tensor]):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+def _plan(key, make):
+    p = _PLANS.get(key)
+    if p is None:
+        p = make()
+        if len(_PLANS) >= _PLANS_MOST:
+            _PLANS.clear()
+        _PLANS[key] = p
+    return p
+
 
 def _on_one_gpu(q: torch.Tensor, *others) -> torch.device:
     """The GPU that holds q; raises unless every tensor given is there."""
@@ -571,28 +594,6 @@ def _on_one_gpu(q: torch.Tensor, *others) -> torch.device:
         if t is not None and t.device != q.device:
             raise ValueError(f"tensors must be on one device, got {q.device} and {t.device}")
     return q.device
-
-
-class _On:
-    """Makes a device current for a call and gives the stream the call is for."""
-
-    def __init__(self, device: torch.device, stream=None):
-        s = stream if stream is not None else torch.cuda.current_stream(device)
-        if s.device != device:
-            raise ValueError(f"the stream is on {s.device}, the tensors on {device}")
-        self.stream = _vp(s.cuda_stream)
-        self.index = device.index
-        self.before = None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.index:
-            self.before = torch.cuda.current_device()
-            torch.cuda.set_device(self.index)
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
 
 
 def _vector(name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> None:
@@ -615,34 +616,80 @@ def _step(t: torch.Tensor, dim: int) -> int:
     return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
-def _plain(name: str, t: torch.Tensor, shape, dtype: torch.dtype) -> None:
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+def _plain(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous()):
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} contiguous, got {t.dtype} {tuple(t.shape)}")
 
 
-def _rope_desc(B, Hq, Hkv, d, T, dtype, freqs, q_weight, k_weight, eps, interleaved, start, new_lens,
-               k_cache, v_cache) -> RopeDesc:
-    """The descriptor without the projections' strides, and the checks the C call cannot make."""
+def _workspace(given: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
+    """The caller's workspace where it is large enough, else a new one."""
+    if given is not None and not given.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    if given is None or given.numel() * given.element_size() < nbytes:
+        return alloc_workspace(nbytes, device)
+    return given
+
+
+def _launch(fn, device: torch.device, stream, *args) -> None:
+    """fn(*args, stream) with the device current; the device's current stream unless one is given."""
+    if stream is None:
+        raw = _raw_stream(device.index)
+    elif stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    else:
+        raw = stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        st = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, raw)
+    if st != ETA_OK:
+        _check(st)
+
+
+# the current stream's handle without building a Stream object (1.5 us of a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _rope_desc(q, k, v, freqs, q_weight, k_weight, eps, interleaved, start, new_lens, k_cache,
+               v_cache) -> RopeDesc:
+    """The descriptor of the forward's tensors, and the checks the C call cannot make."""
+    B, T, Hq, d = q.shape
+    Hkv, dt = k.shape[2], q.dtype
+    _heads_apart("q", q, (B, T, Hq, d), dt)
+    _heads_apart("k", k, (B, T, Hkv, d), dt)
+    _heads_apart("v", v, (B, T, Hkv, d), dt)
     if freqs is not None:
         _vector("freqs", freqs, freqs.numel(), torch.float32)
     _vector("q_weight", q_weight, d, torch.float32)
     _vector("k_weight", k_weight, d, torch.float32)
     _vector("start", start, B, torch.int32)
     _vector("new_lens", new_lens, B, torch.int32)
-    if k_cache.dim() != 4 or k_cache.stride(3) != 1 or k_cache.dtype != dtype or \
-            (k_cache.shape[0], k_cache.shape[1], k_cache.shape[3]) != (B, Hkv, d):
-        raise ValueError(f"the K cache must be {dtype} [{B}][{Hkv}][T_cap][{d}], the head dimension "
-                         f"contiguous, got {k_cache.dtype} {tuple(k_cache.shape)}")
-    if v_cache is not None and (v_cache.shape != k_cache.shape or v_cache.dtype != dtype
-                                or any(_step(v_cache, i) != _step(k_cache, i) for i in range(3))
-                                or v_cache.stride(3) != 1):
+    for c in (k_cache, v_cache):
+        if c is not None and (c.dim() != 4 or c.stride(3) != 1 or c.dtype != dt
+                              or (c.shape[0], c.shape[1], c.shape[3]) != (B, Hkv, d)):
+            raise ValueError(f"a cache must be {dt} [{B}][{Hkv}][T_cap][{d}], the head dimension "
+                             f"contiguous, got {c.dtype} {tuple(c.shape)}")
+    if v_cache is not None and (v_cache.shape != k_cache.shape
+                                or any(_step(v_cache, i) != _step(k_cache, i) for i in range(3))):
         raise ValueError("the K and V caches must share shape, strides and dtype")
-    return RopeDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, new_tokens=T,
-                    dtype=ETA_DT_F32 if dtype == torch.float32 else ETA_DT_BF16,
-                    rotary_dim=0 if freqs is None else 2 * freqs.numel(),
-                    interleaved=int(bool(interleaved)), eps=eps, capacity_tokens=k_cache.shape[2],
-                    cache_stride_b=_step(k_cache, 0), cache_stride_h=_step(k_cache, 1),
-                    cache_stride_t=_step(k_cache, 2))
+    rd = RopeDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, new_tokens=T,
+                  dtype=_dtype_code(q), rotary_dim=0 if freqs is None else 2 * freqs.numel(),
+                  interleaved=int(bool(interleaved)), eps=eps, capacity_tokens=T,
+                  cache_stride_b=Hkv * T * d, cache_stride_h=T * d, cache_stride_t=d,
+                  q_stride_b=_step(q, 0), q_stride_t=_step(q, 1),
+                  k_stride_b=_step(k, 0), k_stride_t=_step(k, 1))
+    if v is not None:
+        rd.v_stride_b, rd.v_stride_t = _step(v, 0), _step(v, 1)
+    if k_cache is not None:
+        rd.capacity_tokens = k_cache.shape[2]
+        rd.cache_stride_b, rd.cache_stride_h, rd.cache_stride_t = (_step(k_cache, i) for i in range(3))
+    return rd
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = None, *,
@@ -659,33 +706,27 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = N
     row start[b] + i; rows of tokens from new_lens[b] on are left as they were.  Caches that are
     not given are allocated with T rows (start must then be None).  Returns (q, k_cache,
     v_cache); for a single token q is what a decode step reads, viewed as [B][Hq][d]."""
-    B, T, Hq, d = q.shape
-    Hkv = k.shape[2]
-    dt = q.dtype
-    _dtype_code(q)
-    dev = _on_one_gpu(q, k, v, freqs, q_weight, k_weight, start, new_lens, q_out, k_cache, v_cache)
-    _heads_apart("q", q, (B, T, Hq, d), dt)
-    _heads_apart("k", k, (B, T, Hkv, d), dt)
-    _heads_apart("v", v, (B, T, Hkv, d), dt)
-    if k_cache is None or (v is not None and v_cache is None):
-        if start is not None or k_cache is not None or v_cache is not None:
+    def make():
+        _dtype_code(q)
+        dev = _on_one_gpu(q, k, v, freqs, q_weight, k_weight, start, new_lens, q_out, k_cache, v_cache)
+        if (k_cache is None or (v is not None and v_cache is None)) and \
+                (start is not None or k_cache is not None or v_cache is not None):
             raise ValueError("start and a cache come with both caches")
-        k_cache = torch.empty(B, Hkv, T, d, device=dev, dtype=dt)
+        if v is None and v_cache is not None:
+            raise ValueError("a V cache comes with v")
+        rd = _rope_desc(q, k, v, freqs, q_weight, k_weight, eps, interleaved, start, new_lens, k_cache, v_cache)
+        _plain("q_out", q_out, (rd.batch, rd.num_q_heads, rd.new_tokens, rd.head_dim), q.dtype)
+        return rd, ctypes.byref(rd), dev
+    rd, ref, dev = _plan((0, eps, interleaved, _form(q), _form(k), _form(v), _form(freqs), _form(q_weight),
+                          _form(k_weight), _form(start), _form(new_lens), _form(q_out), _form(k_cache),
+                          _form(v_cache)), make)
+    if k_cache is None:
+        k_cache = torch.empty(rd.batch, rd.num_kv_heads, rd.new_tokens, rd.head_dim, device=dev, dtype=q.dtype)
         v_cache = None if v is None else torch.empty_like(k_cache)
     if q_out is None:
-        q_out = torch.empty(B, Hq, T, d, device=dev, dtype=dt)
-    _plain("q_out", q_out, (B, Hq, T, d), dt)
-    rd = _rope_desc(B, Hq, Hkv, d, T, dt, freqs, q_weight, k_weight, eps, interleaved, start, new_lens,
-                    k_cache, v_cache if v is not None else None)
-    rd.q_stride_b, rd.q_stride_t = _step(q, 0), _step(q, 1)
-    rd.k_stride_b, rd.k_stride_t = _step(k, 0), _step(k, 1)
-    if v is not None:
-        rd.v_stride_b, rd.v_stride_t = _step(v, 0), _step(v, 1)
-    with _On(dev, stream) as s:
-        _check(load_library().eta_qk_norm_rope(
-            ctypes.byref(rd), _ptr(q), _ptr(k), _ptr(v), _ptr(q_weight), _ptr(k_weight), _ptr(freqs),
-            _ptr(start), _ptr(new_lens), _ptr(q_out), _ptr(k_cache),
-            _ptr(v_cache) if v is not None else None, s))
+        q_out = torch.empty(rd.batch, rd.num_q_heads, rd.new_tokens, rd.head_dim, device=dev, dtype=q.dtype)
+    _launch(load_library().eta_qk_norm_rope, dev, stream, ref, q.data_ptr(), k.data_ptr(), _at(v), _at(q_weight),
+            _at(k_weight), _at(freqs), _at(start), _at(new_lens), q_out.data_ptr(), k_cache.data_ptr(), _at(v_cache))
     return q_out, k_cache, v_cache
 
 
@@ -705,28 +746,35 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_cache: torch.Tensor,
     q, k to (dq, dk, dv, dq_weight, dk_weight).  dq, dk, dv [B][T][H][d] (given: may be views of a
     fused gradient), zero for tokens from new_lens[b] on; the weights' gradients fp32 [d], None
     where the weight is; dv None where dv_cache is."""
-    B, T, Hq, d = q.shape
-    Hkv = k.shape[2]
-    dt = q.dtype
-    _dtype_code(q)
-    dev = _on_one_gpu(q, k, dq_out, dk_cache, dv_cache, freqs, q_weight, k_weight, start, new_lens, dq, dk, dv,
-                      dq_weight, dk_weight, workspace)
-    _heads_apart("q", q, (B, T, Hq, d), dt)
-    _heads_apart("k", k, (B, T, Hkv, d), dt)
-    _plain("dq_out", dq_out, (B, Hq, T, d), dt)
-    rd = _rope_desc(B, Hq, Hkv, d, T, dt, freqs, q_weight, k_weight, eps, interleaved, start, new_lens,
-                    dk_cache, dv_cache)
+    def make():
+        _dtype_code(q)
+        dev = _on_one_gpu(q, k, dq_out, dk_cache, dv_cache, freqs, q_weight, k_weight, start, new_lens, dq, dk, dv,
+                          dq_weight, dk_weight, workspace)
+        rd = _rope_desc(q, k, None, freqs, q_weight, k_weight, eps, interleaved, start, new_lens, dk_cache, dv_cache)
+        B, T, Hq, Hkv, d, dt = rd.batch, rd.new_tokens, rd.num_q_heads, rd.num_kv_heads, rd.head_dim, q.dtype
+        _plain("dq_out", dq_out, (B, Hq, T, d), dt)
+        for name, t, H in (("dq", dq, Hq), ("dk", dk, Hkv), ("dv", dv, Hkv)):
+            _heads_apart(name, t, (B, T, H, d), dt)
+            sb, st = (T * H * d, H * d) if t is None else (_step(t, 0), _step(t, 1))
+            setattr(rd, name + "_stride_b", sb)
+            setattr(rd, name + "_stride_t", st)
+        _vector("dq_weight", dq_weight, d, torch.float32)
+        _vector("dk_weight", dk_weight, d, torch.float32)
+        n = ctypes.c_size_t()
+        _check(load_library().eta_qk_norm_rope_backward_workspace_size(ctypes.byref(rd), ctypes.byref(n)))
+        return rd, ctypes.byref(rd), dev, n.value
+    rd, ref, dev, nbytes = _plan(
+        (1, eps, interleaved, _form(q), _form(k), _form(dq_out), _form(dk_cache), _form(dv_cache), _form(freqs),
+         _form(q_weight), _form(k_weight), _form(start), _form(new_lens), _form(dq), _form(dk), _form(dv),
+         _form(dq_weight), _form(dk_weight), _form(workspace)), make)
     if dq is None:
-        dq = torch.empty(B, T, Hq, d, device=dev, dtype=dt)
+        dq = torch.empty(rd.batch, rd.new_tokens, rd.num_q_heads, rd.head_dim, device=dev, dtype=q.dtype)
     if dk is None:
-        dk = torch.empty(B, T, Hkv, d, device=dev, dtype=dt)
+        dk = torch.empty(rd.batch, rd.new_tokens, rd.num_kv_heads, rd.head_dim, device=dev, dtype=q.dtype)
     if dv_cache is None:
         dv = None
     elif dv is None:
-        dv = torch.empty(B, T, Hkv, d, device=dev, dtype=dt)
-    _heads_apart("dq", dq, (B, T, Hq, d), dt)
-    _heads_apart("dk", dk, (B, T, Hkv, d), dt)
-    _heads_apart("dv", dv, (B, T, Hkv, d), dt)
+        dv = torch.empty(rd.batch, rd.new_tokens, rd.num_kv_heads, rd.head_dim, device=dev, dtype=q.dtype)
     if q_weight is None:
         dq_weight = None
     elif dq_weight is None:
@@ -735,34 +783,12 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_cache: torch.Tensor,
         dk_weight = None
     elif dk_weight is None:
         dk_weight = torch.empty_like(k_weight)
-    _vector("dq_weight", dq_weight, d, torch.float32)
-    _vector("dk_weight", dk_weight, d, torch.float32)
-    rd.q_stride_b, rd.q_stride_t = _step(q, 0), _step(q, 1)
-    rd.k_stride_b, rd.k_stride_t = _step(k, 0), _step(k, 1)
-    rd.dq_stride_b, rd.dq_stride_t = _step(dq, 0), _step(dq, 1)
-    rd.dk_stride_b, rd.dk_stride_t = _step(dk, 0), _step(dk, 1)
-    if dv is not None:
-        rd.dv_stride_b, rd.dv_stride_t = _step(dv, 0), _step(dv, 1)
-    lib = load_library()
-    n = ctypes.c_size_t()
-    _check(lib.eta_qk_norm_rope_backward_workspace_size(ctypes.byref(rd), ctypes.byref(n)))
-    workspace = _workspace(workspace, n.value, dev)
-    with _On(dev, stream) as s:
-        _check(lib.eta_qk_norm_rope_backward(
-            ctypes.byref(rd), _ptr(dq_out), _ptr(dk_cache), _ptr(dv_cache), _ptr(q), _ptr(k),
-            _ptr(q_weight), _ptr(k_weight), _ptr(freqs), _ptr(start), _ptr(new_lens), _ptr(dq),
-            _ptr(dk), _ptr(dv), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), s))
+    workspace = _workspace(workspace, nbytes, dev)
+    _launch(load_library().eta_qk_norm_rope_backward, dev, stream, ref, dq_out.data_ptr(), dk_cache.data_ptr(),
+            _at(dv_cache), q.data_ptr(), k.data_ptr(), _at(q_weight), _at(k_weight), _at(freqs), _at(start),
+            _at(new_lens), dq.data_ptr(), dk.data_ptr(), _at(dv), _at(dq_weight), _at(dk_weight),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return dq, dk, dv, dq_weight, dk_weight
-
-
-def _workspace(given: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
-    """The caller's workspace where it is large enough, else a new one."""
-    if given is not None and not given.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
-    if given is None or given.numel() * given.element_size() < nbytes:
-        return alloc_workspace(nbytes, device)
-    return given
 
 
 def gated_prefill_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: torch.Tensor,
@@ -777,35 +803,37 @@ def gated_prefill_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ta
     additive and C as given to it, out and L as it returned them, dout bf16 [B][Hq][T][d] the
     output's gradient, dR and dL fp32 [B][Hq][T] those of the gate row sums and the log-sum-exp
     (None: zero); returns (dq, dk, dv bf16, dtau fp32), zero past each sequence's end."""
-    B, Hq, T, d = q.shape
-    Hkv = k.shape[1]
-    bf, f32 = torch.bfloat16, torch.float32
-    dev = _on_one_gpu(q, k, v, tau, seq_lens, out, L, dout, dR, dL, dq, dk, dv, dtau, workspace)
-    qs, ks, rs = (B, Hq, T, d), (B, Hkv, T, d), (B, Hq, T)
-    if dq is None:
-        dq = torch.empty(qs, device=dev, dtype=bf)
-    if dk is None:
-        dk = torch.empty(ks, device=dev, dtype=bf)
-    if dv is None:
-        dv = torch.empty(ks, device=dev, dtype=bf)
-    if dtau is None:
-        dtau = torch.empty(rs, device=dev, dtype=f32)
-    for name, t, shape, dt in (("q", q, qs, bf), ("k", k, ks, bf), ("v", v, ks, bf), ("tau", tau, rs, f32),
-                               ("out", out, qs, bf), ("L", L, rs, f32), ("dout", dout, qs, bf),
-                               ("dR", dR, rs, f32), ("dL", dL, rs, f32), ("dq", dq, qs, bf), ("dk", dk, ks, bf),
-                               ("dv", dv, ks, bf), ("dtau", dtau, rs, f32)):
-        if t is not None:
+    def make():
+        dev = _on_one_gpu(q, k, v, tau, seq_lens, out, L, dout, dR, dL, dq, dk, dv, dtau, workspace)
+        B, Hq, T, d = q.shape
+        Hkv = k.shape[1]
+        bf, f32 = torch.bfloat16, torch.float32
+        qs, ks, rs = (B, Hq, T, d), (B, Hkv, T, d), (B, Hq, T)
+        for name, t, shape, dt in (("q", q, qs, bf), ("k", k, ks, bf), ("v", v, ks, bf), ("tau", tau, rs, f32),
+                                   ("out", out, qs, bf), ("L", L, rs, f32), ("dout", dout, qs, bf),
+                                   ("dR", dR, rs, f32), ("dL", dL, rs, f32), ("dq", dq, qs, bf), ("dk", dk, ks, bf),
+                                   ("dv", dv, ks, bf), ("dtau", dtau, rs, f32)):
             _plain(name, t, shape, dt)
-    _vector("seq_lens", seq_lens, B, torch.int32)
-    pd = PrefillDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, capacity_tokens=T,
-                     dtype=ETA_DT_BF16, beta=beta, additive=int(bool(additive)), C=C)
-    lib = load_library()
-    n = ctypes.c_size_t()
-    _check(lib.eta_gated_prefill_backward_workspace_size(ctypes.byref(pd), ctypes.byref(n)))
-    workspace = _workspace(workspace, n.value, dev)
-    with _On(dev, stream) as s:
-        _check(lib.eta_gated_prefill_backward(
-            ctypes.byref(pd), _ptr(q), _ptr(k), _ptr(v), _ptr(tau), _ptr(seq_lens), _ptr(out), _ptr(L),
-            _ptr(dout), _ptr(dR), _ptr(dL), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtau), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), s))
+        _vector("seq_lens", seq_lens, B, torch.int32)
+        pd = PrefillDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, capacity_tokens=T,
+                         dtype=ETA_DT_BF16, beta=beta, additive=int(bool(additive)), C=C)
+        n = ctypes.c_size_t()
+        _check(load_library().eta_gated_prefill_backward_workspace_size(ctypes.byref(pd), ctypes.byref(n)))
+        return pd, ctypes.byref(pd), dev, n.value
+    pd, ref, dev, nbytes = _plan(
+        (2, beta, additive, C, _form(q), _form(k), _form(v), _form(tau), _form(seq_lens), _form(out), _form(L),
+         _form(dout), _form(dR), _form(dL), _form(dq), _form(dk), _form(dv), _form(dtau), _form(workspace)), make)
+    if dq is None:
+        dq = torch.empty_like(q)
+    if dk is None:
+        dk = torch.empty_like(k)
+    if dv is None:
+        dv = torch.empty_like(v)
+    if dtau is None:
+        dtau = torch.empty_like(tau)
+    workspace = _workspace(workspace, nbytes, dev)
+    _launch(load_library().eta_gated_prefill_backward, dev, stream, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            tau.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), L.data_ptr(), dout.data_ptr(), _at(dR), _at(dL),
+            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dtau.data_ptr(), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())
     return dq, dk, dv, dtau
