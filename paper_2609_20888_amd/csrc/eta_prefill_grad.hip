@@ -258,38 +258,50 @@ struct Packer {
   }
 };
 
-// The row scalars (GradArgs::stats): D_i = dO_i.O_i - dL_i, the lanes of a row 16 bytes each.  Rows at or past
-// the sequence's end, up to a whole block, get P = 0 and no gradient.  Bound by reading O and dO.
+// The row scalars (GradArgs::stats): D_i = dO_i.O_i - dL_i, the lanes of a row 16 bytes each, 64 rows of a head a
+// workgroup.  Rows at or past the sequence's end, up to a whole block, get P = 0 and no gradient.  Bound by
+// reading O and dO.
 template <int D>
 __global__ __launch_bounds__(256) void grad_rows_kernel(GradArgs a) {
-  constexpr int LPR = D / 8, RPW = 256 / LPR;
-  const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / LPR;      // (Tp is a multiple of RPW)
-  const int64_t head = row / a.Tp;
-  const int t = (int)(row - head * a.Tp), c = threadIdx.x % LPR;
-  const bool in = t < (int)clamp_len(a.seq_lens, (int)(head / a.Hq), a.T);
-  const int64_t at = head * a.T + (in ? t : 0);
-  float s = 0.f;
-  if (in) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(a.dout + at * D + 8 * c), y = *reinterpret_cast<const u32x4*>(a.out + at * D + 8 * c);
+  constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;       // lanes of a row, rows of a pass, passes
+  __shared__ float d_s[64];
+  const int blk = (int)(blockIdx.x % (uint32_t)(a.Tp / 64));
+  const int64_t head = blockIdx.x / (uint32_t)(a.Tp / 64);
+  const int n = (int)clamp_len(a.seq_lens, (int)(head / a.Hq), a.T) - 64 * blk;   // rows of the block that count
+  const int r = threadIdx.x / LPR, c = threadIdx.x % LPR;
+  const int64_t row0 = head * a.T + 64 * blk;
+  u32x4 x[NP], y[NP];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
-      s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+  for (int i = 0; i < NP; ++i) {
+    const int64_t at = (row0 + r + RPP * i) * D + 8 * c;
+    x[i] = y[i] = u32x4{0, 0, 0, 0};
+    if (r + RPP * i < n) {
+      x[i] = *reinterpret_cast<const u32x4*>(a.dout + at);
+      y[i] = *reinterpret_cast<const u32x4*>(a.out + at);
     }
   }
-  s = lanes_sum<LPR>(s);
-  if (c < 4) {
-    float v = c == 0 ? kNegInf : 0.f;
-    if (in) {
-      if (c == 0) v = -a.L[at] * kLog2e;
-      if (c == 1) v = a.beta * kLog2e * a.tau[at];
-      if (c == 2) v = a.dL ? a.dL[at] - s : -s;
-      if (c == 3) v = a.dR ? a.beta * a.dR[at] : 0.f;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s = fmaf(__uint_as_float(x[i][j] << 16), __uint_as_float(y[i][j] << 16), s);
+      s = fmaf(__uint_as_float(x[i][j] & 0xffff0000u), __uint_as_float(y[i][j] & 0xffff0000u), s);
     }
-    const float s2 = kLog2e / sqrtf((float)D);
-    if (c == 1) v -= log2f(s2);
-    a.stats[(head * a.Tp + (t & ~31)) * 4 + 32 * c + (t & 31)] = v;
+    s = lanes_sum<LPR>(s);
+    if (c == 0) d_s[r + RPP * i] = s;
   }
+  __syncthreads();
+  const int which = threadIdx.x >> 6, t = threadIdx.x & 63;        // one scalar of 64 rows a wavefront
+  float v = which == 0 ? kNegInf : 0.f;
+  if (t < n) {
+    if (which == 0) v = -a.L[row0 + t] * kLog2e;
+    if (which == 1) v = a.beta * kLog2e * a.tau[row0 + t];
+    if (which == 2) v = a.dL ? a.dL[row0 + t] - d_s[t] : -d_s[t];
+    if (which == 3) v = a.dR ? a.beta * a.dR[row0 + t] : 0.f;
+  }
+  if (which == 1) v -= log2f(kLog2e / sqrtf((float)D));
+  a.stats[(head * a.Tp + 64 * blk + (t & 32)) * 4 + 32 * which + (t & 31)] = v;
 }
 
 // dq, dtau of 128 query rows.  As in the forward each lane owns a query row: S^T = K Q^T and dP^T =
@@ -697,8 +709,9 @@ hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, 
   a.C = pd.additive ? pd.C : 0.f;
   hipError_t e = with_hook(hook, ETA_KERNEL_PREFILL_GRAD_ROWS, stream, [&] {
     const int64_t rows = (int64_t)pd.batch * pd.num_q_heads * p.rows;
-    if (pd.head_dim == 64) hipLaunchKernelGGL((grad_rows_kernel<64>), dim3((uint32_t)(rows / 32)), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((grad_rows_kernel<128>), dim3((uint32_t)(rows / 16)), dim3(256), 0, stream, a);
+    const dim3 grid((uint32_t)(rows / 64));
+    if (pd.head_dim == 64) hipLaunchKernelGGL((grad_rows_kernel<64>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((grad_rows_kernel<128>), grid, dim3(256), 0, stream, a);
   });
   if (e != hipSuccess) return e;
   const dim3 grid((uint32_t)((int64_t)p.blocks * pd.batch * (pd.num_q_heads + pd.num_kv_heads * p.nsplit)));
