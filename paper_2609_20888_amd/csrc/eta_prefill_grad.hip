@@ -78,19 +78,19 @@ struct RowScalars {
 
 // The vector work of a unit: 16 scores of a lane, raw products in s and dO.v - D in dp, two
 // scores a step, the four stages of a score one step apart so that no step waits for its own
-// transcendentals; the last stage, the first to read dp, DL steps after the first.  row(j) gives score j's scalars, mask(j, valid, diag) its place (MASKED),
+// transcendentals.  row(j) gives score j's scalars, mask(j, valid, diag) its place (MASKED),
 // done(j, p, ds, n) takes P, s2 dS and s2 sg' m (the last with TAU only); beside(step) is the matrix work of a step.
-template <int DL, bool ADD, bool MASKED, bool TAU, typename Row, typename Mask, typename Done, typename Beside>
+template <bool ADD, bool MASKED, bool TAU, typename Row, typename Mask, typename Done, typename Beside>
 __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, const f32x16& dp, Row row, Mask mask,
                                             Done done, Beside beside) {
   float e[16], u[16], w[16], p[16];       // (a few of each are alive at a time)
 #pragma unroll
-  for (int st = 0; st < 8 + DL; ++st) {
+  for (int st = 0; st < 11; ++st) {
     beside(st);
-    if (st >= DL) {
+    if (st >= 3) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int j = 2 * (st - DL) + i, o = j;
+        const int j = 2 * (st - 3) + i, o = j;
         const float d = p[o] * dp[j], kap = row(j).kap;
         float m = fmaf(ADD ? d : d * s[j], g.kd, kap), lin = ADD ? g.s2 : u[o];
         if constexpr (MASKED) {
@@ -179,7 +179,7 @@ struct Tile {
   static constexpr int NR = 4;                       // row addresses of a lane
   static __device__ __forceinline__ int swizzle(int row) {
     if constexpr (D == 128) return (row & 3) << 2;
-    return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1);
+    return ((row >> 1) & 1) << 2;
   }
   static __device__ __forceinline__ uint32_t at(int row, int chunk) {
     return (uint32_t)(row / GR * GB + row % GR * 2 * D + 16 * (chunk ^ swizzle(row)));
@@ -373,7 +373,7 @@ __device__ __forceinline__ void grad_q(const GradArgs& a, char* lds, int qblk, i
     }
     Packer pk;
     float un = 0.f;
-    unit_scores<3, ADD, MASKED, true>(
+    unit_scores<ADD, MASKED, true>(
         g, s, dp, [&](int) { return rs; },
         [&](int i, bool& valid, bool& diag) {
           const int j = u * 32 + 8 * (i >> 2) + 4 * g2 + (i & 3);
@@ -463,7 +463,7 @@ template <int D>
 struct KeyWalk {
   static constexpr bool VLDS = D == 128;
   static constexpr int TR = D == 128 ? 32 : 64, UT = TR / 32;      // rows and units of a tile
-  static constexpr int NKL = VLDS ? 2 : 0;                         // K operands kept in LDS
+  static constexpr int NKL = VLDS ? 3 : 0;                         // K operands kept in LDS
   static constexpr int TILE = UT * Tile<D>::HALF, BUF = 2 * TILE + 4 * TR * 4;
   static constexpr int VB = VLDS ? 4 * (D / 16 + NKL) * 1024 : 0;
   static constexpr int LDS = VB + 2 * BUF;                         // V (and K operands), then twice: Q, dO, row scalars
@@ -526,43 +526,60 @@ __device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, 
   for (int db = 0; db < DB; ++db) ta[db] = lds_address(lds) + VB + TL::turn_base(lane, db);
   const uint32_t sa = lds_address(lds) + VB + 2 * TILE + 16 * g2;
 
-  // One unit of 32 query rows, the tile's half at byte offset `at` of its buffer.
-  constexpr int LA = 4;                                            // LDS operands ahead of their MFMA
+  // One unit of 32 query rows (half a tile where the tile has 64).  Its MFMAs in order: S, dP, the
+  // products into dv and dk, those of the rows whose P and dS come first beside the last steps of the
+  // vector work.  (The rest overlaps with the vector work of the SIMD's other wavefront.)
+  constexpr int LA = 3;                                            // LDS operands ahead of their MFMA
+  constexpr int NM = 2 * KC + 4 * DB;
   auto unit = [&](int row0, int buf, int half, auto masked_tag) {
     constexpr bool MASKED = decltype(masked_tag)::value;
     const int at = buf * BUF + half * TL::HALF;
     auto scalars = [&](int which, int x) {                         // rows 8 x + 4 g2 .. + 3
       return lds_floats(sa + buf * BUF + half * 512 + which * 128 + 32 * x);
     };
-    u32x4 op[LA], ov[2], ok[NKL ? NKL : 1];
+    u32x4 op[LA], ov[LA];
     f32x16 s{}, dp;
+    Packer pp, pd;
+    auto rd = [&](int x) {
+      if (x < 2 * KC) {
+        const int kc = x % KC;
+        op[x % LA] = lds_rows(ra[kc / TL::PER] + at + (x < KC ? 0 : TILE) + TL::row_step(kc));
+        if (x < NKL) ov[x % LA] = lds_rows(va + (KC + kc) * 1024);
+        if (VLDS && x >= KC) ov[x % LA] = lds_rows(va + kc * 1024);
+      } else if (x < NM) {
+        const int y = x - 2 * KC, c = y / (2 * DB), db = y % (2 * DB) / 2;
+        const uint32_t o = ta[db] + at + (y & 1 ? 0 : TILE);
+        op[x % LA] = lds_turned(o + TL::turn_step(c, 0), o + TL::turn_step(c, 1));
+      }
+    };
+    auto step = [&](int x) {
+      if (x < KC) {
+        s = mfma(op[x % LA], x < NKL ? ov[x % LA] : kf[x < NKL ? 0 : x - NKL], s);
+      } else if (x < 2 * KC) {
+        dp = mfma(op[x % LA], VLDS ? ov[x % LA] : vf[VLDS ? 0 : x - KC], dp);
+      } else {
+        const int y = x - 2 * KC, c = y / (2 * DB), db = y % (2 * DB) / 2;
+        if (y & 1) dka[db] = mfma(op[x % LA], pd.o[c], dka[db]);
+        else dva[db] = mfma(op[x % LA], pp.o[c], dva[db]);
+      }
+      rd(x + LA);
+    };
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const f32x4 nd = scalars(2, x);
 #pragma unroll
       for (int i = 0; i < 4; ++i) dp[4 * x + i] = nd[i];
     }
-    auto rd = [&](int x) {
-      const int kc = x >> 1;
-      if (x >= 2 * KC) return;
-      op[x % LA] = lds_rows(ra[kc / TL::PER] + at + (x & 1 ? TILE : 0) + TL::row_step(kc));
-      if (VLDS && (x & 1)) ov[kc & 1] = lds_rows(va + kc * 1024);
-      if (!(x & 1) && kc < NKL) ok[kc] = lds_rows(va + (KC + kc) * 1024);
-    };
 #pragma unroll
     for (int x = 0; x < LA; ++x) rd(x);
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) {
-      if (x & 1) dp = mfma(op[x % LA], VLDS ? ov[(x >> 1) & 1] : vf[VLDS ? 0 : x >> 1], dp);
-      else s = mfma(op[x % LA], (x >> 1) < NKL ? ok[(x >> 1) % (NKL ? NKL : 1)] : kf[(x >> 1) - NKL], s);
-      rd(x + LA);
+      step(x);
       __builtin_amdgcn_sched_barrier(0);
     }
-    Packer pp, pd;
     f32x4 nl[4], bt[4], kap[4];
     bt[0] = scalars(1, 0);
-    constexpr int DL = 3;
-    unit_scores<DL, ADD, MASKED, false>(
+    unit_scores<ADD, MASKED, false>(
         g, s, dp, [&](int i) { return RowScalars{bt[i >> 2][i & 3], nl[i >> 2][i & 3], kap[i >> 2][i & 3]}; },
         [&](int i, bool& valid, bool& diag) {
           const int row = row0 + 8 * (i >> 2) + 4 * g2 + (i & 3);
@@ -576,22 +593,14 @@ __device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, 
         [&](int st) {        // the scalars of four rows are read a step before the first of them is due
           if (st % 2 == 1 && st < 7) bt[(st + 1) / 2] = scalars(1, (st + 1) / 2);
           if (st % 2 == 1 && st < 8) nl[st / 2] = scalars(0, st / 2);
-          if (st >= DL - 1 && (st - DL + 1) % 2 == 0 && st < DL + 7) kap[(st - DL + 1) / 2] = scalars(3, (st - DL + 1) / 2);
+          if (st >= 2 && st % 2 == 0 && st < 10) kap[st / 2 - 1] = scalars(3, st / 2 - 1);
+#pragma unroll
+          for (int x = 2 * KC; x < 2 * KC + 2 * DB; ++x)           // (the first half is packed in step 6)
+            if (7 + (x - 2 * KC) * 4 / (2 * DB) == st) step(x);
         });
-    auto rt = [&](int x) {
-      const int c = x / (2 * DB), db = x % (2 * DB) / 2;
-      if (x >= 4 * DB) return;
-      const uint32_t o = ta[db] + at + (x & 1 ? 0 : TILE);
-      op[x % LA] = lds_turned(o + TL::turn_step(c, 0), o + TL::turn_step(c, 1));
-    };
 #pragma unroll
-    for (int x = 0; x < LA; ++x) rt(x);
-#pragma unroll
-    for (int x = 0; x < 4 * DB; ++x) {
-      const int c = x / (2 * DB), db = x % (2 * DB) / 2;
-      if (x & 1) dka[db] = mfma(op[x % LA], pd.o[c], dka[db]);
-      else dva[db] = mfma(op[x % LA], pp.o[c], dva[db]);
-      rt(x + LA);
+    for (int x = 2 * KC + 2 * DB; x < NM; ++x) {
+      step(x);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
