@@ -40,7 +40,7 @@ struct GradArgs {
   const int32_t* seq_lens;
   uint16_t *dq, *dk, *dv;
   float* dtau;
-  float* stats;              // [B Hq][Tp / 32][4][32]: -L', beta tau' + log2 is2, -D, beta dR
+  float* stats;              // [B Hq][Tp / 32][4][32]: -L', beta tau' + log2(kd is2), -D, sqrt(d) dR or dR (Gate)
   float* part;               // [2][nsplit][B Hkv][T][d] partial dk, dv (nsplit > 1)
   int64_t part_step;         // nsplit B Hkv T d
   int B, Hq, Hkv, T, Tp, nsplit;
@@ -51,27 +51,30 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 extern "C" __device__ float eta_mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
 
-// A score's gate and gradient, in base-2 units (S' = S log2 e = s2 c, c the raw product):
-// E = is2 2^(-beta (S' - tau')) (the factor is2 = 1 / s2 is in the exponent), u = 1 / (E + is2)
-// = s2 sg, u E = 1 - sg, so sg' keeps its relative accuracy where the gate is nearly open or
-// nearly shut (the legacy product gives 0 for 0 x inf, the shut gate).
+// A score's gate and gradient, in base-2 units (S' = S log2 e = s2 c, c the raw product), with kd = beta /
+// sqrt(d) (additive: beta), the factor of m, folded into the exponential:
+//   E = kd is2 2^(-beta (S' - tau')) (is2 = 1 / s2),  u = 1 / (E / kd + is2) = s2 sg,  u E = kd (1 - sg),
+//   m / kd = c dS~ + sqrt(d) dR (additive: C dS~ + dR),  s2 sg' m = u (u E) (m / kd).
+// sg' keeps its relative accuracy where the gate is nearly open or nearly shut (the legacy product
+// gives 0 for 0 x inf, the shut gate).
 struct Gate {
-  float s2, is2, nbs, lis2, kd, C2, C2is;   // kd: beta / sqrt(d) (additive: beta C)
-  template <int D>
-  static __device__ __forceinline__ Gate make(float beta, float C, bool add) {
+  float s2, is2, nbs, kd, ikd, C, C2, C2is;
+  template <int D, bool ADD>
+  static __device__ __forceinline__ Gate make(float beta, float C) {
     Gate g;
     g.s2 = kLog2e / sqrtf((float)D);
     g.is2 = 1.0f / g.s2;
     g.nbs = -beta * g.s2;
-    g.lis2 = log2f(g.is2);
-    g.kd = add ? beta * C : beta / sqrtf((float)D);
+    g.kd = fmaxf(beta, 1e-30f) * (ADD ? 1.0f : 1.0f / sqrtf((float)D));     // (beta 0: m's share is far below any other)
+    g.ikd = 1.0f / g.kd;
+    g.C = C;
     g.C2 = C * kLog2e;
     g.C2is = g.C2 * g.is2;
     return g;
   }
 };
 
-// The row scalars of a score: t: beta tau' + log2 is2; nl: -L'; kap: beta dR.
+// The row scalars of a score: t: beta tau' + log2(kd is2); nl: -L'; kap: sqrt(d) dR (additive: dR).
 struct RowScalars {
   float t, nl, kap;
 };
@@ -92,7 +95,7 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
       for (int i = 0; i < 2; ++i) {
         const int j = 2 * (st - 3) + i, o = j;
         const float d = p[o] * dp[j], kap = row(j).kap;
-        float m = fmaf(ADD ? d : d * s[j], g.kd, kap), lin = ADD ? g.s2 : u[o];
+        float m = fmaf(d, ADD ? g.C : s[j], kap), lin = ADD ? g.s2 : u[o];
         if constexpr (MASKED) {
           bool valid, diag;
           mask(j, valid, diag);
@@ -109,7 +112,7 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int j = 2 * (st - 2) + i, o = j;
-        w[o] = eta_mul_legacy(u[o], e[o]);              // 1 - sg
+        w[o] = eta_mul_legacy(u[o], e[o]);              // kd (1 - sg)
         if constexpr (TAU || ADD || MASKED) w[o] *= u[o];
         const float nl = row(j).nl;
         float y = ADD ? fmaf(g.C2is, u[o], fmaf(s[j], g.s2, nl - g.C2)) : fmaf(s[j], u[o], nl);
@@ -126,7 +129,7 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int o = 2 * (st - 1) + i;
-        u[o] = __builtin_amdgcn_rcpf(e[o] + g.is2);
+        u[o] = __builtin_amdgcn_rcpf(fmaf(e[o], g.ikd, g.is2));
       }
     }
     if (st < 8) {
@@ -261,7 +264,7 @@ struct Packer {
 // The row scalars (GradArgs::stats): D_i = dO_i.O_i - dL_i, the lanes of a row 16 bytes each, 64 rows of a head a
 // workgroup.  Rows at or past the sequence's end, up to a whole block, get P = 0 and no gradient.  Bound by
 // reading O and dO.
-template <int D>
+template <int D, bool ADD>
 __global__ __launch_bounds__(256) void grad_rows_kernel(GradArgs a) {
   constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;       // lanes of a row, rows of a pass, passes
   __shared__ float d_s[64];
@@ -298,9 +301,12 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(GradArgs a) {
     if (which == 0) v = -a.L[row0 + t] * kLog2e;
     if (which == 1) v = a.beta * kLog2e * a.tau[row0 + t];
     if (which == 2) v = a.dL ? a.dL[row0 + t] - d_s[t] : -d_s[t];
-    if (which == 3) v = a.dR ? a.beta * a.dR[row0 + t] : 0.f;
+    if (which == 3) v = a.dR ? a.dR[row0 + t] * (ADD ? 1.0f : sqrtf((float)D)) : 0.f;
   }
-  if (which == 1) v -= log2f(kLog2e / sqrtf((float)D));
+  if (which == 1) {
+    const Gate g = Gate::make<D, ADD>(a.beta, a.C);
+    v += log2f(g.kd * g.is2);
+  }
   a.stats[(head * a.Tp + 64 * blk + (t & 32)) * 4 + 32 * which + (t & 31)] = v;
 }
 
@@ -319,7 +325,7 @@ __device__ __forceinline__ void grad_q(const GradArgs& a, char* lds, int qblk, i
   const int Tb = (int)clamp_len(a.seq_lens, b, a.T);
   const int64_t head = (int64_t)b * a.Hq + h, qrow0 = head * a.T;
   const int64_t kvoff = ((int64_t)b * a.Hkv + h / (a.Hq / a.Hkv)) * a.T * D;
-  const Gate g = Gate::make<D>(a.beta, a.C, ADD);
+  const Gate g = Gate::make<D, ADD>(a.beta, a.C);
 
   const int wrow0 = qblk * kGrQ + 32 * w, t = wrow0 + r32, tq = min(t, max(Tb, 1) - 1);
   u32x4 qb[KC], dob[KC];
@@ -445,7 +451,7 @@ __device__ __forceinline__ void grad_q(const GradArgs& a, char* lds, int qblk, i
         const uint32_t hi = in ? pack_bf16x2(acc[db][i + 2] * kLn2, acc[db][i + 3] * kLn2) : 0u;
         *reinterpret_cast<uint2*>(a.dq + (qrow0 + t) * D + 32 * db + 2 * i + 4 * g2) = make_uint2(lo, hi);
       }
-    if (g2 == 0) a.dtau[qrow0 + t] = in ? -nsum * g.is2 : 0.f;
+    if (g2 == 0) a.dtau[qrow0 + t] = in && a.beta != 0.f ? -nsum * g.is2 : 0.f;
   }
 }
 
@@ -480,7 +486,7 @@ __device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, 
   const int r32 = lane & 31, g2 = lane >> 5;
   const int Tb = (int)clamp_len(a.seq_lens, b, a.T);
   const int GH = a.Hq / a.Hkv / a.nsplit, h0 = kvh * (a.Hq / a.Hkv) + split * GH;   // this workgroup's heads
-  const Gate g = Gate::make<D>(a.beta, a.C, ADD);
+  const Gate g = Gate::make<D, ADD>(a.beta, a.C);
   const int wrow0 = kblk * kGrQ + 32 * w, j = wrow0 + r32, jk = min(j, max(Tb, 1) - 1);
   const int64_t kvrow0 = ((int64_t)b * a.Hkv + kvh) * a.T;
   u32x4 kf[KC - NKL], vf[VLDS ? 1 : KC];
@@ -719,8 +725,13 @@ hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, 
   hipError_t e = with_hook(hook, ETA_KERNEL_PREFILL_GRAD_ROWS, stream, [&] {
     const int64_t rows = (int64_t)pd.batch * pd.num_q_heads * p.rows;
     const dim3 grid((uint32_t)(rows / 64));
-    if (pd.head_dim == 64) hipLaunchKernelGGL((grad_rows_kernel<64>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((grad_rows_kernel<128>), grid, dim3(256), 0, stream, a);
+    if (pd.additive) {
+      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_rows_kernel<64, true>), grid, dim3(256), 0, stream, a);
+      else hipLaunchKernelGGL((grad_rows_kernel<128, true>), grid, dim3(256), 0, stream, a);
+    } else {
+      if (pd.head_dim == 64) hipLaunchKernelGGL((grad_rows_kernel<64, false>), grid, dim3(256), 0, stream, a);
+      else hipLaunchKernelGGL((grad_rows_kernel<128, false>), grid, dim3(256), 0, stream, a);
+    }
   });
   if (e != hipSuccess) return e;
   const dim3 grid((uint32_t)((int64_t)p.blocks * pd.batch * (pd.num_q_heads + pd.num_kv_heads * p.nsplit)));
