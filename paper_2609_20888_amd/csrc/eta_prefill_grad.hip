@@ -143,20 +143,35 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
   }
 }
 
-// The work of a workgroup: blocks of 128 rows by length of their walk, the longest first, and at
-// each length all (key head, head split, sequence) then all (query head, sequence).  With a multiple of
-// eight heads neighbouring heads, which share K and V, are on one XCD (workgroups are dealt to the
-// eight XCDs round robin).
+// The work of a workgroup, the longest walks first.  A rank is a block of 128 rows, rank 0 the one
+// with the longest walk, of all (key head, head split, sequence) or of all (query head, sequence); a walk of
+// the keys is as long as that of `heads` ranks of queries.  So the first ranks are the keys', and then
+// come groups of one rank of theirs and `heads` of the queries'.  With a multiple of eight heads
+// neighbouring heads, which share K and V, are on one XCD (workgroups are dealt to the eight XCDs
+// round robin).
 struct GradWork {
   bool keys;
   int blk, h, b;             // h: query head, or key head * nsplit + split
 };
 __device__ __forceinline__ GradWork grad_work(const GradArgs& a, uint32_t wg, int blocks) {
-  const uint32_t nk = (uint32_t)(a.Hkv * a.nsplit * a.B), nq = (uint32_t)(a.Hq * a.B), rank = wg / (nk + nq);
-  uint32_t i = wg % (nk + nq);
+  const uint32_t nk = (uint32_t)(a.Hkv * a.nsplit * a.B), nq = (uint32_t)(a.Hq * a.B);
+  const uint32_t heads = (uint32_t)(a.Hq / a.Hkv / a.nsplit), first = (uint32_t)blocks - ((uint32_t)blocks + heads - 1) / heads;
+  uint32_t rank, i;
   GradWork x;
-  x.keys = i < nk;
-  if (!x.keys) i -= nk;
+  if (wg < first * nk) {
+    x.keys = true;
+    rank = wg / nk;
+    i = wg % nk;
+  } else {
+    const uint32_t in = wg - first * nk, group = in / (nk + heads * nq);
+    i = in % (nk + heads * nq);
+    x.keys = i < nk;
+    rank = first + group;
+    if (!x.keys) {
+      rank = group * heads + (i - nk) / nq;
+      i = (i - nk) % nq;
+    }
+  }
   x.blk = x.keys ? (int)rank : blocks - 1 - (int)rank;
   const uint32_t H = (uint32_t)(x.keys ? a.Hkv * a.nsplit : a.Hq);
   if ((H & 7) == 0) {
