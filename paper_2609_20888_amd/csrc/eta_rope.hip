@@ -27,7 +27,9 @@ namespace {
 // backward: 125 -> 108 us; 4 x 2000, 32/4, d = 64, fp32: 46.5 -> 42.6 us).  The forward writes with it
 // too (STREAM) where the call's bytes pass what the last-level cache holds beside other work: 246 MB
 // 56 -> 52 us, 403 MB 88 -> 81 us; at 202 MB the two are equal, and below that what is written is
-// best left in the cache for its reader (fp32, 147 MB: 28 us, with the hint 30).
+// best left in the cache for its reader (fp32, 147 MB: 28 us, with the hint 30).  The backward, which
+// writes a third of its bytes, does so from further on: 570 MB 126 -> 116 us where each call has other
+// result buffers; 188 MB 46 us, with the hint 52.
 typedef uint32_t u32x4n __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 get16(const char* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(p)));
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 // dw stay in a lane's registers over all its rows; a workgroup adds its token groups in
 // order and leaves one row of partials, which rope_weight_kernel adds in order, so the
 // result does not depend on the order of the workgroups.
-template <typename T, int D>
+template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
   constexpr int E = Piece<T>::E, LPR = D / E, TPW = 256 / LPR;
   constexpr int64_t ROW = D * sizeof(T);
@@ -337,7 +339,7 @@ __global__ __launch_bounds__(256) void rope_grad_kernel(RopeArgs a) {
           res = Piece<T>::pack(g);
         }
         if (!live) res = make_uint4(0, 0, 0, 0);
-        if (in_range && h + u < sh.h1) put16<false>(out + (h + u) * ROW, res);
+        if (in_range && h + u < sh.h1) put16<STREAM>(out + (h + u) * ROW, res);
       }
     }
   }
@@ -425,16 +427,16 @@ RopeArgs rope_args(const eta_rope_desc_t& rd, const RopePlan& p, const float* qw
   return a;
 }
 
-// Launches a kernel for the descriptor's type and head dimension (further template arguments after these).
-#define ETA_ROPE_LAUNCH(kernel, ...)                                                                                    \
-  do {                                                                                                                  \
-    if (rd.dtype == ETA_DT_F32) {                                                                                       \
-      if (rd.head_dim == 64) hipLaunchKernelGGL((kernel<float, 64 __VA_ARGS__>), grid, dim3(256), 0, stream, a);        \
-      else hipLaunchKernelGGL((kernel<float, 128 __VA_ARGS__>), grid, dim3(256), 0, stream, a);                         \
-    } else {                                                                                                            \
-      if (rd.head_dim == 64) hipLaunchKernelGGL((kernel<uint16_t, 64 __VA_ARGS__>), grid, dim3(256), 0, stream, a);     \
-      else hipLaunchKernelGGL((kernel<uint16_t, 128 __VA_ARGS__>), grid, dim3(256), 0, stream, a);                      \
-    }                                                                                                                   \
+// Launches a kernel for the descriptor's type and head dimension.
+#define ETA_ROPE_LAUNCH(kernel, STREAM)                                                                         \
+  do {                                                                                                          \
+    if (rd.dtype == ETA_DT_F32) {                                                                               \
+      if (rd.head_dim == 64) hipLaunchKernelGGL((kernel<float, 64, STREAM>), grid, dim3(256), 0, stream, a);    \
+      else hipLaunchKernelGGL((kernel<float, 128, STREAM>), grid, dim3(256), 0, stream, a);                     \
+    } else {                                                                                                    \
+      if (rd.head_dim == 64) hipLaunchKernelGGL((kernel<uint16_t, 64, STREAM>), grid, dim3(256), 0, stream, a); \
+      else hipLaunchKernelGGL((kernel<uint16_t, 128, STREAM>), grid, dim3(256), 0, stream, a);                  \
+    }                                                                                                           \
   } while (0)
 
 }  // namespace
@@ -452,8 +454,8 @@ hipError_t launch_rope(const eta_rope_desc_t& rd, const RopePlan& p, const void*
   a.v_out = (char*)v_cache;
   const dim3 grid(p.tiles, p.nq + p.nk + p.nv);
   return with_hook(hook, ETA_KERNEL_QK_ROPE, stream, [&] {
-    if (p.stream) ETA_ROPE_LAUNCH(rope_kernel, , true);
-    else ETA_ROPE_LAUNCH(rope_kernel, , false);
+    if (p.stream) ETA_ROPE_LAUNCH(rope_kernel, true);
+    else ETA_ROPE_LAUNCH(rope_kernel, false);
   });
 }
 
@@ -475,7 +477,8 @@ hipError_t launch_rope_grad(const eta_rope_desc_t& rd, const RopePlan& p, const 
   a.part = part;
   const dim3 grid(p.steps, p.nq + p.nk + p.nv);
   hipError_t e = with_hook(hook, ETA_KERNEL_QK_ROPE_GRAD, stream, [&] {
-    ETA_ROPE_LAUNCH(rope_grad_kernel);
+    if (p.stream) ETA_ROPE_LAUNCH(rope_grad_kernel, true);
+    else ETA_ROPE_LAUNCH(rope_grad_kernel, false);
   });
   if (e != hipSuccess || (!qw && !kw)) return e;
   return with_hook(hook, ETA_KERNEL_QK_WEIGHT_GRAD, stream, [&] {

@@ -113,7 +113,7 @@ RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad) {
   const int most = kRopePartials / p.nq;      // nq >= nk, nq <= 256
   p.steps = grad && p.tiles > most ? most : p.tiles;
   const int64_t rows = (int64_t)rd.batch * rd.new_tokens * (rd.num_q_heads + rd.num_kv_heads * (has_v ? 2 : 1));
-  p.stream = !grad && rows * rd.head_dim * elem_bytes(rd.dtype) * 2 > (int64_t(200) << 20);
+  p.stream = rows * rd.head_dim * elem_bytes(rd.dtype) * (grad ? 3 : 2) > (int64_t(grad ? 480 : 200) << 20);
   return p;
 }
 

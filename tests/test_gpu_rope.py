@@ -251,6 +251,53 @@ def test_cache_past_32_bits():
     assert (kc[:, :, -4] == 7).all() and (vc[:, :, -4] == 7).all()
 
 
+@pytest.mark.parametrize("lens", [[20011], [9000, 11011]])
+def test_long_sequences(lens):
+    """Calls whose bytes pass the last-level cache (results written past it): sampled tokens, V whole,
+    and the weights' gradients against sums in 64 bits on the GPU."""
+    Hq, Hkv, d, T, B = 32, 8, 128, max(lens), len(lens)
+    gen = torch.Generator(device="cuda").manual_seed(len(lens))
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(BF)  # noqa: E731
+    x = rnd(B, T, Hq + 2 * Hkv, d)
+    q, k, v = x[:, :, :Hq], x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:]
+    freqs = (10000.0 ** (-torch.arange(0, d, 2).double() / d)).float()
+    qw, kw = (1 + 0.3 * torch.randn(d, generator=gen, device="cuda") for _ in range(2))
+    args = dict(freqs=freqs.cuda(), q_weight=qw, k_weight=kw, eps=EPS,
+                new_lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    qo, kc, vc = eta.qk_norm_rope(q, k, v, **args)
+    gq, gk, gv = rnd(B, Hq, T, d), rnd(B, Hkv, T, d), rnd(B, Hkv, T, d)
+    dq, dk, dv, dqw, dkw = eta.qk_norm_rope_backward(gq, gk, gv, q, k, **args)
+    torch.cuda.synchronize()
+    hs = rs.half_step(BF)
+    for b, n in enumerate(lens):
+        assert torch.equal(vc[b, :, :n].transpose(0, 1), v[b, :n])
+        assert torch.equal(dv[b, :n], gv[b, :, :n].transpose(0, 1))
+        assert not dq[b, n:].any() and not dk[b, n:].any() and not dv[b, n:].any()
+        at = torch.cat([torch.arange(0, n, 311), torch.tensor([n - 1])])
+        for inp, w, out, gy, dx in ((q, qw, qo, gq, dq), (k, kw, kc, gk, dk)):
+            xs, ws = inp[b, at.cuda()].cpu(), w.cpu()
+            y, tol = rs.forward(xs, ws, at, freqs, False, EPS)
+            got = out[b][:, at.cuda()].cpu().transpose(0, 1).double()
+            assert ((got - y).abs() <= tol + hs * (y.abs() + tol)).all()
+            y, tol, _, _ = rs.backward(xs, ws, gy[b][:, at.cuda()].cpu().transpose(0, 1), at, freqs, False, EPS)
+            assert ((dx[b, at.cuda()].cpu().double() - y).abs() <= tol + hs * (y.abs() + tol)).all()
+    # every term is off by at most 24 U of its size and a sum of independent terms by far less than their
+    # number: 24 U of the sizes' sum plus the chains of up to 512 terms, added 16 and 64 at a time
+    for inp, gy, dw in ((q, gq, dqw), (k, gk, dkw)):
+        total, size = 0.0, 0.0
+        for b, n in enumerate(lens):
+            for h in range(inp.shape[2]):
+                xs = inp[b, :n, h].double()
+                nrm = xs * (xs.square().mean(-1, keepdim=True) + EPS).rsqrt()
+                a = torch.arange(n, device="cuda").double()[:, None] * freqs.cuda().double()
+                g, c, s = gy[b, h, :n].double(), torch.cos(a), torch.sin(a)
+                u, w = g[:, :d // 2], g[:, d // 2:]
+                turned = torch.cat([u * c + w * s, w * c - u * s], 1)
+                total = total + (turned * nrm).sum(0)
+                size = size + (torch.cat([u.abs() + w.abs()] * 2, 1) * nrm.abs()).sum(0)
+        assert ((dw.double() - total).abs() <= (24 + 512 + 80) * rs.U * size).all()
+
+
 def test_two_graphs_and_another_stream():
     """Two captured gradient passes with workspaces of their own, replayed with new inputs and
     eager work between the replays; and a call on another stream."""
