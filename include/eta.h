@@ -417,7 +417,8 @@ eta_status_t eta_gated_prefill(const eta_prefill_desc_t* pd, const void* q, cons
  * dk and dv over every query head of the kv head's group.  Products on the matrix cores
  * (bf16 operands, fp32 accumulation; P and dS are rounded to bf16 for theirs), everything
  * else fp32; sums in a fixed order (bitwise reproducible).
- *   pd          as for the forward; capacity_tokens <= 2^24
+ *   pd          as for the forward; capacity_tokens <= 2^24, and batch * num_q_heads *
+ *               capacity_tokens, rounded up to 128 tokens, below 2^30
  *   q, k, v, tau, seq_lens   the forward's inputs
  *   out, L      the forward's results for them
  *   dout        bf16, like out;  dR, dL  fp32, like R and L, or NULL (zero)
@@ -465,7 +466,7 @@ typedef struct {
   int32_t num_q_heads;
   int32_t num_kv_heads;        /* num_q_heads / num_kv_heads in {1, 2, 4, 8}; num_q_heads <= 256 */
   int32_t head_dim;            /* 64 or 128 */
-  int32_t new_tokens;          /* >= 1; batch * new_tokens < 2^31 - 64 */
+  int32_t new_tokens;          /* >= 1; batch * new_tokens <= 2^26 */
   int32_t dtype;               /* of q, k, v, the caches and their gradients */
   int32_t rotary_dim;          /* a multiple of 16 in [0, head_dim]; 0: norm only */
   int32_t interleaved;         /* 0 or 1 */
@@ -483,7 +484,8 @@ typedef struct {
  *   q_weight, k_weight   fp32 [head_dim], or NULL
  *   freqs        fp32 [rotary_dim / 2]; may be NULL when rotary_dim is 0
  *   q_out        [batch][num_q_heads][new_tokens][head_dim], contiguous
- * q_out and the caches must not overlap q, k and v.
+ * q_out and the caches must not overlap q, k and v, and no two rows of a cache may share an
+ * element (in the backward: no two rows of dq, dk or dv).
  */
 eta_status_t eta_qk_norm_rope(const eta_rope_desc_t* rd, const void* q, const void* k, const void* v,
                               const float* q_weight, const float* k_weight, const float* freqs,

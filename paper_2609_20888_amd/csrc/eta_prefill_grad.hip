@@ -10,6 +10,7 @@
 #include "eta_lanes.h"
 #include "eta_tile.h"
 #include "eta_train.h"
+#include "eta_train_index.h"
 
 namespace eta {
 namespace {
@@ -141,48 +142,6 @@ __device__ __forceinline__ void unit_scores(const Gate& g, const f32x16& s, cons
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-}
-
-// The work of a workgroup, the longest walks first.  A rank is a block of 128 rows, rank 0 the one
-// with the longest walk, of all (key head, head split, sequence) or of all (query head, sequence); a walk of
-// the keys is as long as that of `heads` ranks of queries.  So the first ranks are the keys', and then
-// come groups of one rank of theirs and `heads` of the queries'.  With a multiple of eight heads
-// neighbouring heads, which share K and V, are on one XCD (workgroups are dealt to the eight XCDs
-// round robin).
-struct GradWork {
-  bool keys;
-  int blk, h, b;             // h: query head, or key head * nsplit + split
-};
-__device__ __forceinline__ GradWork grad_work(const GradArgs& a, uint32_t wg, int blocks) {
-  const uint32_t nk = (uint32_t)(a.Hkv * a.nsplit * a.B), nq = (uint32_t)(a.Hq * a.B);
-  const uint32_t heads = (uint32_t)(a.Hq / a.Hkv / a.nsplit), first = (uint32_t)blocks - ((uint32_t)blocks + heads - 1) / heads;
-  uint32_t rank, i;
-  GradWork x;
-  if (wg < first * nk) {
-    x.keys = true;
-    rank = wg / nk;
-    i = wg % nk;
-  } else {
-    const uint32_t in = wg - first * nk, group = in / (nk + heads * nq);
-    i = in % (nk + heads * nq);
-    x.keys = i < nk;
-    rank = first + group;
-    if (!x.keys) {
-      rank = group * heads + (i - nk) / nq;
-      i = (i - nk) % nq;
-    }
-  }
-  x.blk = x.keys ? (int)rank : blocks - 1 - (int)rank;
-  const uint32_t H = (uint32_t)(x.keys ? a.Hkv * a.nsplit : a.Hq);
-  if ((H & 7) == 0) {
-    const uint32_t hpx = H / 8, r = i / 8;
-    x.h = (int)((i % 8) * hpx + r % hpx);
-    x.b = (int)(r / hpx);
-  } else {
-    x.h = (int)(i % H);
-    x.b = (int)(i / H);
-  }
-  return x;
 }
 
 // A tile of rows of D bf16 in LDS: groups of 1 KiB (what a wavefront's direct load writes), 16 bytes
@@ -660,6 +619,9 @@ __device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, 
     }
   }
 
+  if (j >= Tb)       // (no pair reached these sums; a NaN of the sequence's last row, which stood in for the key, may have)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) dka[db] = dva[db] = f32x16{};
   if (j < a.T) {
     if (a.nsplit > 1) {
       float* o = a.part + (((int64_t)(split * a.B + b) * a.Hkv + kvh) * a.T + j) * D + 4 * g2;
@@ -690,7 +652,7 @@ __device__ __forceinline__ void grad_kv(const GradArgs& a, char* lds, int kblk, 
 template <int D, bool ADD>
 __global__ __launch_bounds__(256, 2) void grad_kernel(GradArgs a, int blocks) {
   __shared__ __attribute__((aligned(16))) char lds[kGradQLds<D> > KeyWalk<D>::LDS ? kGradQLds<D> : KeyWalk<D>::LDS];
-  const GradWork x = grad_work(a, blockIdx.x, blocks);
+  const GradWork x = grad_work(blockIdx.x, (uint32_t)blocks, (uint32_t)a.B, (uint32_t)a.Hq, (uint32_t)a.Hkv, (uint32_t)a.nsplit);
   if (x.keys) grad_kv<D, ADD>(a, lds, x.blk, x.h, x.b);
   else grad_q<D, ADD>(a, lds, x.blk, x.h, x.b);
 }

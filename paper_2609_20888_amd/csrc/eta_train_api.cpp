@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "eta.h"
@@ -39,8 +40,9 @@ eta_status_t check_rope(const eta_rope_desc_t* rd) {
   if (!rd) return fail(ETA_ERR_INVALID_ARG, "rotation descriptor is NULL");
   if (rd->batch < 1 || rd->new_tokens < 1 || rd->capacity_tokens < 1)
     return fail(ETA_ERR_INVALID_ARG, "batch, new_tokens and capacity_tokens must be >= 1");
-  if ((int64_t)rd->batch * rd->new_tokens >= (int64_t(1) << 31) - 64)
-    return fail(ETA_ERR_UNSUPPORTED, "batch * new_tokens must stay below 2^31 - 64");
+  // (at least eight tokens a workgroup, and fewer than 2^24 workgroups of 256 threads along a grid)
+  if ((int64_t)rd->batch * rd->new_tokens > (int64_t(1) << 26))
+    return fail(ETA_ERR_UNSUPPORTED, "batch * new_tokens must not exceed 2^26");
   if (eta_status_t st = check_heads(rd->num_q_heads, rd->num_kv_heads, rd->head_dim)) return st;
   if (!valid_dtype(rd->dtype)) return fail(ETA_ERR_INVALID_ARG, "dtype %d is not ETA_DT_F32 or ETA_DT_BF16", rd->dtype);
   if (rd->rotary_dim < 0 || rd->rotary_dim > rd->head_dim || rd->rotary_dim % 16 != 0)
@@ -51,15 +53,31 @@ eta_status_t check_rope(const eta_rope_desc_t* rd) {
   return ETA_OK;
 }
 
-// Strides of a projection [batch][new_tokens][heads][head_dim].  What is written may not
-// overlap itself: there neighbouring tokens and sequences must be a row of heads apart.
+// Whether the dimensions (size, stride) around rows of `row` elements are nested, so that no two of
+// their rows share an element: what is written must be.
+struct Dim {
+  int64_t size, stride;
+};
+bool nested(int64_t row, Dim* dims, int n) {
+  std::sort(dims, dims + n, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  int64_t extent = row;
+  for (int i = 0; i < n; ++i) {
+    if (dims[i].size <= 1) continue;
+    if (dims[i].stride < extent) return false;
+    extent += dims[i].stride * (dims[i].size - 1);
+  }
+  return true;
+}
+
+// Strides of a projection [batch][new_tokens][heads][head_dim].
 eta_status_t check_rows(const eta_rope_desc_t& rd, const char* what, int heads, int64_t sb, int64_t st,
                         bool written) {
   const int64_t eb = elem_bytes(rd.dtype), row = (int64_t)heads * rd.head_dim;
   if (sb < 0 || st < 0) return fail(ETA_ERR_INVALID_ARG, "%s: negative stride", what);
   if ((sb * eb) % 16 || (st * eb) % 16)
     return fail(ETA_ERR_INVALID_ARG, "%s: strides must keep rows 16-byte aligned", what);
-  if (written && ((rd.new_tokens > 1 && st < row) || (rd.batch > 1 && sb < row)))
+  Dim dims[] = {{rd.batch, sb}, {rd.new_tokens, st}};
+  if (written && !nested(row, dims, 2))
     return fail(ETA_ERR_INVALID_ARG, "%s: rows that are written overlap", what);
   return ETA_OK;
 }
@@ -72,7 +90,8 @@ eta_status_t check_cache(const eta_rope_desc_t& rd, bool written) {
     return fail(ETA_ERR_INVALID_ARG, "cache: strides must keep token rows 16-byte aligned");
   if (st < d && rd.capacity_tokens > 1)
     return fail(ETA_ERR_INVALID_ARG, "cache_stride_t (%lld) < head_dim (%d)", (long long)st, rd.head_dim);
-  if (written && ((rd.num_kv_heads > 1 && sh < d) || (rd.batch > 1 && sb < d)))
+  Dim dims[] = {{rd.batch, sb}, {rd.num_kv_heads, sh}, {rd.capacity_tokens, st}};
+  if (written && !nested(d, dims, 3))
     return fail(ETA_ERR_INVALID_ARG, "cache: rows that are written overlap");
   return ETA_OK;
 }
@@ -83,6 +102,9 @@ eta_status_t check_prefill(const eta_prefill_desc_t* pd) {
     return fail(ETA_ERR_INVALID_ARG, "batch must be in [1, 65535] and capacity_tokens >= 1");
   if (pd->capacity_tokens > (1 << 24)) return fail(ETA_ERR_UNSUPPORTED, "capacity_tokens > 2^24 unsupported");
   if (eta_status_t st = check_heads(pd->num_q_heads, pd->num_kv_heads, pd->head_dim)) return st;
+  // (fewer than 2^24 workgroups of 256 threads along a grid: 64 rows each, rows in blocks of 128)
+  if (((int64_t)pd->capacity_tokens + 127) / 128 * 128 * pd->batch * pd->num_q_heads >= (int64_t(1) << 30))
+    return fail(ETA_ERR_UNSUPPORTED, "batch * num_q_heads * capacity_tokens, rounded up to 128 tokens, must stay below 2^30");
   if (pd->dtype != ETA_DT_BF16) return fail(ETA_ERR_UNSUPPORTED, "the prefill's gradients take bf16 q, k, v");
   if (!std::isfinite(pd->beta) || pd->beta < 0.f)
     return fail(ETA_ERR_INVALID_ARG, "beta must be finite and >= 0");
@@ -117,6 +139,10 @@ RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad) {
   return p;
 }
 
+// The heads of a group are split while the workgroups of 128 keys do not fill two per compute unit: the
+// longest walk of a workgroup is otherwise the call's time (4096 tokens, 16/4 heads, d = 128: 698 us whole,
+// 422 split in two, 336 in four; 2 x 2048: 349, 212, 174).  From there on the partials cost more than the
+// walks gain (8192 tokens: 1122 us in two, 1218 in four; 4 x 2000, 32/4, d = 64: 440, 466).
 GradPlan plan_prefill_grad(const eta_prefill_desc_t& pd) {
   GradPlan p;
   p.blocks = (pd.capacity_tokens + 127) / 128;

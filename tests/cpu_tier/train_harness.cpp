@@ -11,6 +11,7 @@
 #include "eta.h"
 #include "eta_host.h"
 #include "eta_train.h"
+#include "eta_train_index.h"
 
 static int failures = 0, launches = 0;
 static size_t g_bytes = 0;                            // of the call's workspace
@@ -78,6 +79,27 @@ hipError_t launch_prefill_grad(const eta_prefill_desc_t& pd, const GradPlan& p, 
   const int G = pd.num_q_heads / pd.num_kv_heads;
   CHECK(p.nsplit >= 1 && G % p.nsplit == 0, "split %d of %d heads", p.nsplit, G);
   CHECK(p.rows % 128 == 0 && p.rows >= pd.capacity_tokens && p.rows < pd.capacity_tokens + 128, "rows %d", p.rows);
+  // every (kind, block, head, sequence) is one workgroup's, and along the launch neither kind's walks
+  // get longer
+  const uint32_t nk = (uint32_t)(pd.num_kv_heads * p.nsplit * pd.batch), nq = (uint32_t)(pd.num_q_heads * pd.batch);
+  const uint32_t wgs = (nk + nq) * (uint32_t)p.blocks;
+  if (wgs < 300000) {
+    std::vector<char> seen(wgs);
+    int last[2] = {p.blocks - 1, 0};
+    for (uint32_t wg = 0; wg < wgs; ++wg) {
+      const GradWork x = grad_work(wg, (uint32_t)p.blocks, (uint32_t)pd.batch, (uint32_t)pd.num_q_heads,
+                                   (uint32_t)pd.num_kv_heads, (uint32_t)p.nsplit);
+      const int H = x.keys ? pd.num_kv_heads * p.nsplit : pd.num_q_heads;
+      const bool ok = x.blk >= 0 && x.blk < p.blocks && x.h >= 0 && x.h < H && x.b >= 0 && x.b < pd.batch;
+      CHECK(ok, "workgroup %u: block %d head %d sequence %d", wg, x.blk, x.h, x.b);
+      if (!ok) break;
+      const size_t at = (x.keys ? 0 : (size_t)nk * p.blocks) + ((size_t)x.blk * pd.batch + x.b) * H + x.h;
+      CHECK(!seen[at], "workgroup %u repeats", wg);
+      seen[at] = 1;
+      CHECK(x.keys ? x.blk >= last[1] : x.blk <= last[0], "workgroup %u: a longer walk later", wg);
+      last[x.keys] = x.blk;
+    }
+  }
   const size_t stats = (size_t)4 * pd.batch * pd.num_q_heads * p.rows * 4;
   const size_t part = p.nsplit == 1 ? 0 : (size_t)2 * p.nsplit * pd.batch * pd.num_kv_heads * pd.capacity_tokens * pd.head_dim * 4;
   std::memset(x.stats, 1, 64);

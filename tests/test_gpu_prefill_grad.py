@@ -268,3 +268,17 @@ def test_another_stream():
     st.wait_stream(torch.cuda.current_stream())
     for a, b in zip(run(c, stream=st), want):
         assert torch.equal(a, b)
+
+
+def test_last_row_not_finite():
+    """A NaN in the last row of a sequence's K or V stands in for no row past its end: their gradients
+    stay zero, and so do the other sequence's results as they were."""
+    c = make(2, 4, 2, 128, 90, lens=[70, 90], seed=12)
+    clean = run(c)
+    c["k"][0, :, 69] = float("nan")
+    c["v"][0, :, 69, 3] = float("inf")
+    dq, dk, dv, dtau = run(c)
+    assert (dk[0, :, 70:] == 0).all() and (dv[0, :, 70:] == 0).all()
+    assert (dq[0, :, 70:] == 0).all() and (dtau[0, :, 70:] == 0).all()
+    for a, b in zip((dq, dk, dv, dtau), clean):
+        assert torch.equal(a[1], b[1])

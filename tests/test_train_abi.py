@@ -42,7 +42,7 @@ def rope_grad(lib, desc=None, **kw):
 
 BAD_ROPE = [
     (dict(batch=0), INVALID), (dict(new_tokens=0), INVALID), (dict(capacity_tokens=0), INVALID),
-    (dict(batch=1 << 16, new_tokens=1 << 15), UNSUPPORTED), (dict(num_kv_heads=3), INVALID),
+    (dict(batch=1 << 14, new_tokens=(1 << 12) + 1), UNSUPPORTED), (dict(num_kv_heads=3), INVALID),
     (dict(num_q_heads=32), UNSUPPORTED), (dict(num_q_heads=512, num_kv_heads=64), UNSUPPORTED),
     (dict(head_dim=96), UNSUPPORTED), (dict(dtype=eta.ETA_DT_F16), INVALID), (dict(rotary_dim=8), INVALID),
     (dict(rotary_dim=144), INVALID), (dict(rotary_dim=-16), INVALID), (dict(interleaved=2), INVALID),
@@ -72,9 +72,11 @@ def test_rope_grad_pointers_refused(lib, kw):
 
 def test_rope_strides_refused(lib):
     for kw in (dict(q_stride_t=-8), dict(k_stride_b=4), dict(v_stride_t=12), dict(cache_stride_t=64),
-               dict(cache_stride_h=-128), dict(cache_stride_b=0), dict(cache_stride_h=64), dict(cache_stride_t=132)):
+               dict(cache_stride_h=-128), dict(cache_stride_b=0), dict(cache_stride_h=64), dict(cache_stride_t=132),
+               dict(cache_stride_h=128), dict(cache_stride_b=64 * 128), dict(cache_stride_b=2 * 128, cache_stride_t=128)):
         assert rope(lib, rope_desc(**kw)) == INVALID, kw
-    for kw in (dict(dq_stride_t=512), dict(dk_stride_b=128), dict(dv_stride_t=0), dict(dq_stride_b=4), dict(k_stride_t=-8)):
+    for kw in (dict(dq_stride_t=512), dict(dk_stride_b=128), dict(dv_stride_t=0), dict(dq_stride_b=4), dict(k_stride_t=-8),
+               dict(dq_stride_b=1024)):
         assert rope_grad(lib, rope_desc(**kw)) == INVALID, kw
 
 
@@ -125,6 +127,7 @@ def prefill_grad(lib, desc=None, **kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(batch=0), INVALID), (dict(batch=65536), INVALID), (dict(capacity_tokens=0), INVALID),
     (dict(capacity_tokens=(1 << 24) + 1), UNSUPPORTED), (dict(num_kv_heads=3), INVALID),
+    (dict(batch=65535, num_q_heads=256, num_kv_heads=256, capacity_tokens=1), UNSUPPORTED),
     (dict(num_q_heads=32), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(dtype=eta.ETA_DT_F32), UNSUPPORTED),
     (dict(beta=-1.0), INVALID), (dict(beta=float("inf")), INVALID), (dict(additive=2), INVALID),
     (dict(additive=1, C=float("nan")), INVALID)])
@@ -155,3 +158,11 @@ def test_binding_refuses_prefill_tensors_on_the_host():
     x, r = torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 3)
     with pytest.raises(ValueError, match="GPU"):
         eta.gated_prefill_backward(x, x, x, r, torch.zeros(1, dtype=torch.int32), x, r, x, beta=4.0)
+
+
+def test_rope_other_layouts_accepted_by_the_checks(lib):
+    """Token-major caches and projections with the batch inside pass every stride check (the call then
+    stops at the missing workspace, before anything is enqueued)."""
+    d = rope_desc(cache_stride_b=64 * 256, cache_stride_t=256, cache_stride_h=128, dq_stride_b=1024, dq_stride_t=2048,
+                  dk_stride_b=256, dk_stride_t=512, dv_stride_b=256, dv_stride_t=512)
+    assert rope_grad(lib, d, ws=None) == WORKSPACE
