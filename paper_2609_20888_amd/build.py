@@ -39,7 +39,8 @@ def hipcc() -> str:
 
 # MFMA results kept in the ordinary vector registers: for the prefill kernel only
 # (no copies between accumulation and arithmetic registers there; the
-# calibration kernel is faster with the default register classes)
+# calibration kernel is faster with the default register classes, and the
+# prefill's gradients, at 256 registers a wavefront, get the same code from them)
 VGPR_FORM = {"eta_prefill.hip"}
 
 

@@ -29,8 +29,11 @@ namespace {
 // keys, in an order that changes).  Both kinds run in one launch, the longest walks first, so that
 // short ones fill the compute units beside the last long ones; the row scalars that both read (D
 // among them) come from a small launch before.
-// What bounds it: vector-ALU issue, as in the forward (three transcendentals and about a dozen
-// other instructions for a score of either kind).
+// What bounds it: vector-ALU issue (three transcendentals and 10 to 12 other instructions for a score of
+// either kind; 84% of the time at d = 64) and at d = 128 the card's power: 16K tokens, 32/8 heads:
+// 8.3 ms, 660 TFLOP/s of the five products and 925 of the seven that run (a plain library product:
+// 1260), the vector unit 69% and the matrix cores 52% busy at 1.85 GHz.  d = 64: 5.3 ms.  4096
+// tokens, 16/4 heads, d = 128: 335 us.
 
 constexpr int kGrQ = 128;    // rows (queries or keys) a workgroup owns, 32 per wavefront
 constexpr int kGrT = 64;     // rows of a streamed tile
