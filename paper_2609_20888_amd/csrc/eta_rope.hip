@@ -210,6 +210,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     return;
   }
   const float* wt = sh.kind == 0 ? a.qw : a.kw;
+  // the first rows are on their way while the sines are formed
+  uint4 r[kRopeAhead];
+  auto fetch = [&](int h) {
+#pragma unroll
+    for (int u = 0; u < kRopeAhead; ++u) r[u] = get16(in + min(h + u, sh.h1 - 1) * ROW);
+  };
+  fetch(sh.h0);
   Turn<E, LPR> turn;
   turn.set(a, chunk, lane, t.row);
   float w[E], wo[E];              // weights of the lane's values and of their pairs' others
@@ -221,10 +228,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     w[e] *= turn.c[e];
   }
   for (int h = sh.h0; h < sh.h1; h += kRopeAhead) {
-    uint4 r[kRopeAhead];
-#pragma unroll
-    for (int u = 0; u < kRopeAhead; ++u)
-      r[u] = get16(in + min(h + u, sh.h1 - 1) * ROW);
+    if (h > sh.h0) fetch(h);
 #pragma unroll
     for (int u = 0; u < kRopeAhead; ++u) {
       float x[E], o[E];
