@@ -33,7 +33,7 @@ namespace {
 // either kind; 84% of the time at d = 64) and at d = 128 the card's power: 16K tokens, 32/8 heads:
 // 8.3 ms, 660 TFLOP/s of the five products and 925 of the seven that run (a plain library product:
 // 1260), the vector unit 69% and the matrix cores 52% busy at 1.85 GHz.  d = 64: 5.3 ms.  4096
-// tokens, 16/4 heads, d = 128: 335 us.
+// tokens, 16/4 heads, d = 128: 315 us.
 
 constexpr int kGrQ = 128;    // rows (queries or keys) a workgroup owns, 32 per wavefront
 constexpr int kGrT = 64;     // rows of a streamed tile
