@@ -229,6 +229,29 @@ def decode_params(*, beta=4.0, z=1.0, offset_a=0.0, rescue_window=128, lwb=0,
                         screen_all=int(bool(screen_all)), num_splits=num_splits)
 
 
+# A call with ``stream=`` runs there, beside the current stream's work (its inputs are the caller's to
+# order), and may still run when it has returned.  What it allocates therefore comes from that stream's part of torch's caching
+# allocator: a block of the current stream's may still be read by work queued there, and a
+# workspace given back to it could be handed out again while the call's kernels use it.
+
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A result of a call on ``stream`` (None: the current one), which the current stream may use
+    too once it has waited for that one."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _new_workspace(nbytes: int, device, stream) -> torch.Tensor:
+    if stream is None:
+        return alloc_workspace(nbytes, device)
+    with torch.cuda.stream(stream):
+        return alloc_workspace(nbytes, device)
+
+
 # ---------------------------------------------------------------- entry points
 
 def build_block_summaries(k: torch.Tensor, seq_lens: torch.Tensor, block_size: int, *,
@@ -621,12 +644,12 @@ def _plain(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> N
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} contiguous, got {t.dtype} {tuple(t.shape)}")
 
 
-def _workspace(given: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
+def _workspace(given: Optional[torch.Tensor], nbytes: int, device, stream) -> torch.Tensor:
     """The caller's workspace where it is large enough, else a new one."""
     if given is not None and not given.is_contiguous():
         raise ValueError("the workspace must be contiguous")
     if given is None or given.numel() * given.element_size() < nbytes:
-        return alloc_workspace(nbytes, device)
+        return _new_workspace(nbytes, device, stream)
     return given
 
 
@@ -721,10 +744,11 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = N
                           _form(k_weight), _form(start), _form(new_lens), _form(q_out), _form(k_cache),
                           _form(v_cache)), make)
     if k_cache is None:
-        k_cache = torch.empty(rd.batch, rd.num_kv_heads, rd.new_tokens, rd.head_dim, device=dev, dtype=q.dtype)
-        v_cache = None if v is None else torch.empty_like(k_cache)
+        shape = (rd.batch, rd.num_kv_heads, rd.new_tokens, rd.head_dim)
+        k_cache = _empty(shape, q.dtype, dev, stream)
+        v_cache = None if v is None else _empty(shape, q.dtype, dev, stream)
     if q_out is None:
-        q_out = torch.empty(rd.batch, rd.num_q_heads, rd.new_tokens, rd.head_dim, device=dev, dtype=q.dtype)
+        q_out = _empty((rd.batch, rd.num_q_heads, rd.new_tokens, rd.head_dim), q.dtype, dev, stream)
     _launch(load_library().eta_qk_norm_rope, dev, stream, ref, q.data_ptr(), k.data_ptr(), _at(v), _at(q_weight),
             _at(k_weight), _at(freqs), _at(start), _at(new_lens), q_out.data_ptr(), k_cache.data_ptr(), _at(v_cache))
     return q_out, k_cache, v_cache
@@ -768,22 +792,22 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_cache: torch.Tensor,
          _form(q_weight), _form(k_weight), _form(start), _form(new_lens), _form(dq), _form(dk), _form(dv),
          _form(dq_weight), _form(dk_weight), _form(workspace)), make)
     if dq is None:
-        dq = torch.empty(rd.batch, rd.new_tokens, rd.num_q_heads, rd.head_dim, device=dev, dtype=q.dtype)
+        dq = _empty((rd.batch, rd.new_tokens, rd.num_q_heads, rd.head_dim), q.dtype, dev, stream)
     if dk is None:
-        dk = torch.empty(rd.batch, rd.new_tokens, rd.num_kv_heads, rd.head_dim, device=dev, dtype=q.dtype)
+        dk = _empty((rd.batch, rd.new_tokens, rd.num_kv_heads, rd.head_dim), q.dtype, dev, stream)
     if dv_cache is None:
         dv = None
     elif dv is None:
-        dv = torch.empty(rd.batch, rd.new_tokens, rd.num_kv_heads, rd.head_dim, device=dev, dtype=q.dtype)
+        dv = _empty((rd.batch, rd.new_tokens, rd.num_kv_heads, rd.head_dim), q.dtype, dev, stream)
     if q_weight is None:
         dq_weight = None
     elif dq_weight is None:
-        dq_weight = torch.empty_like(q_weight)
+        dq_weight = _empty((rd.head_dim,), torch.float32, dev, stream)
     if k_weight is None:
         dk_weight = None
     elif dk_weight is None:
-        dk_weight = torch.empty_like(k_weight)
-    workspace = _workspace(workspace, nbytes, dev)
+        dk_weight = _empty((rd.head_dim,), torch.float32, dev, stream)
+    workspace = _workspace(workspace, nbytes, dev, stream)
     _launch(load_library().eta_qk_norm_rope_backward, dev, stream, ref, dq_out.data_ptr(), dk_cache.data_ptr(),
             _at(dv_cache), q.data_ptr(), k.data_ptr(), _at(q_weight), _at(k_weight), _at(freqs), _at(start),
             _at(new_lens), dq.data_ptr(), dk.data_ptr(), _at(dv), _at(dq_weight), _at(dk_weight),
@@ -824,14 +848,14 @@ def gated_prefill_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ta
         (2, beta, additive, C, _form(q), _form(k), _form(v), _form(tau), _form(seq_lens), _form(out), _form(L),
          _form(dout), _form(dR), _form(dL), _form(dq), _form(dk), _form(dv), _form(dtau), _form(workspace)), make)
     if dq is None:
-        dq = torch.empty_like(q)
+        dq = _empty(q.shape, q.dtype, dev, stream)
     if dk is None:
-        dk = torch.empty_like(k)
+        dk = _empty(k.shape, k.dtype, dev, stream)
     if dv is None:
-        dv = torch.empty_like(v)
+        dv = _empty(v.shape, v.dtype, dev, stream)
     if dtau is None:
-        dtau = torch.empty_like(tau)
-    workspace = _workspace(workspace, nbytes, dev)
+        dtau = _empty(tau.shape, tau.dtype, dev, stream)
+    workspace = _workspace(workspace, nbytes, dev, stream)
     _launch(load_library().eta_gated_prefill_backward, dev, stream, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             tau.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), L.data_ptr(), dout.data_ptr(), _at(dR), _at(dL),
             dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dtau.data_ptr(), workspace.data_ptr(),

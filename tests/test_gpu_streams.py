@@ -1,0 +1,91 @@
+"""Calls on a given stream while the current one goes on: what the call allocated is neither
+handed out again nor still in other use while its kernels run; needs an MI355X."""
+import pytest
+import torch
+
+from gpu_support import require_gpu, say
+from paper_2609_20888_amd import eta
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def _gpu(request):
+    require_gpu()
+    say(f"\n[gpu] {request.node.nodeid}")
+    yield
+    torch.cuda.synchronize()
+
+
+def beside(call):
+    """call(stream=...) queued behind a wait on another stream, with buffers of every size that it
+    may have allocated taken, filled and given back on the current stream meanwhile, twice; against
+    the same call on the current stream."""
+    torch.cuda.synchronize()
+    want = [t.clone() for t in call(None) if t is not None]
+    torch.cuda.synchronize()
+    for _ in range(2):
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            torch.cuda._sleep(20_000_000)             # (about 10 ms, so that the fills come first)
+        got = [t for t in call(st) if t is not None]
+        for n in range(8, 27):
+            for _ in range(3):
+                torch.empty(1 << n, dtype=torch.uint8, device="cuda").fill_(255)
+        torch.cuda.current_stream().wait_stream(st)
+        assert len(got) == len(want)
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), i
+
+
+def rope_inputs(B=2, Hq=8, Hkv=2, d=128, T=300):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x = r(B, T, Hq + 2 * Hkv, d).to(BF)
+    kw = dict(freqs=(10000.0 ** (-torch.arange(0, d, 2).double() / d)).float().cuda(), q_weight=1 + 0.3 * r(d),
+              k_weight=1 + 0.3 * r(d))
+    return (x[:, :, :Hq], x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:]), kw, r
+
+
+def prefill_inputs(B=2, Hq=8, Hkv=2, d=64, T=400):
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    q, k, v, dout = (r(B, h, T, d).to(BF) for h in (Hq, Hkv, Hkv, Hq))
+    return q, k, v, 0.5 + 0.5 * r(B, Hq, T), torch.tensor([T, T - 77], dtype=torch.int32, device="cuda"), dout
+
+
+def test_rotation():
+    (q, k, v), kw, _ = rope_inputs()
+    beside(lambda st: eta.qk_norm_rope(q, k, v, stream=st, **kw))
+
+
+def test_rotation_gradients():
+    (q, k, v), kw, r = rope_inputs()
+    gq, gk, gv = (r(2, h, 300, 128).to(BF) for h in (8, 2, 2))
+    beside(lambda st: eta.qk_norm_rope_backward(gq, gk, gv, q, k, stream=st, **kw))
+
+
+def test_prefill_gradients():
+    q, k, v, tau, lens, dout = prefill_inputs()
+    out, _, L = eta.gated_prefill(q, k, v, tau, lens, beta=4.0)
+    beside(lambda st: eta.gated_prefill_backward(q, k, v, tau, lens, out, L, dout, beta=4.0, stream=st))
+
+
+def test_two_streams_at_once():
+    """Two calls queued on two streams at the same time, each with a workspace of its own."""
+    q, k, v, tau, lens, dout = prefill_inputs()
+    out, _, L = eta.gated_prefill(q, k, v, tau, lens, beta=4.0)
+    args = [(q, k, v, tau, lens, out, L, x) for x in (dout, -2 * dout)]
+    want = [eta.gated_prefill_backward(*a, beta=4.0) for a in args]
+    streams = [torch.cuda.Stream() for _ in args]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            torch.cuda._sleep(20_000_000)
+    got = [eta.gated_prefill_backward(*a, beta=4.0, stream=st) for a, st in zip(args, streams)]
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for a, b in zip(g, w):
+            assert torch.equal(a, b)
