@@ -7,6 +7,7 @@ fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -241,7 +242,7 @@ def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream(device))
+    _shared(stream, t)
     return t
 
 
@@ -250,6 +251,13 @@ def _new_workspace(nbytes: int, device, stream) -> torch.Tensor:
         return alloc_workspace(nbytes, device)
     with torch.cuda.stream(stream):
         return alloc_workspace(nbytes, device)
+
+
+def _shared(stream, *tensors: torch.Tensor) -> None:
+    """The caller's stream uses tensors that were allocated on the one given."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(torch.cuda.current_stream(t.device))
 
 
 # ---------------------------------------------------------------- entry points
@@ -265,7 +273,9 @@ def build_block_summaries(k: torch.Tensor, seq_lens: torch.Tensor, block_size: i
     B, Hkv, T_cap, d = k.shape
     desc = kv_desc(k, num_q_heads or Hkv, block_size)
     if out is None:
-        out = Summaries.empty(B, Hkv, d, T_cap // block_size, k.device, stat_dtype)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = Summaries.empty(B, Hkv, d, T_cap // block_size, k.device, stat_dtype)
+        _shared(stream, out.mu, out.sigma, out.max_norm)
     sd = out.desc()
     lib = load_library()
     if sub_block:
@@ -313,7 +323,7 @@ def predict_threshold(q: torch.Tensor, W: Optional[torch.Tensor], bias: torch.Te
     B, Hq, d = q.shape
     _check_predictor(q, W, bias)
     if out is None:
-        out = torch.empty(B, Hq, device=q.device, dtype=torch.float32)
+        out = _empty((B, Hq), torch.float32, q.device, stream)
     _check(load_library().eta_predict_threshold(B, Hq, d, _dtype_code(q), _ptr(q), _ptr(W),
                                                 _ptr(bias), _ptr(out), _stream(stream)))
     return out
@@ -342,16 +352,16 @@ class DecodeOut:
     union_counts: Optional[torch.Tensor] = None  # [B][Hkv] int32 GQA union blocks
 
 
-def _decode_outputs(q, k, summ, out, mask, counts, union_counts, want_counts):
+def _decode_outputs(q, k, summ, out, mask, counts, union_counts, want_counts, stream):
     B, Hq, _ = q.shape
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if mask is None:
-        mask = torch.empty(B, Hq, summ.n_blk_cap, dtype=torch.uint8, device=q.device)
+        mask = _empty((B, Hq, summ.n_blk_cap), torch.uint8, q.device, stream)
     if counts is None and want_counts:
-        counts = torch.empty(B, Hq, dtype=torch.int32, device=q.device)
+        counts = _empty((B, Hq), torch.int32, q.device, stream)
     if union_counts is None and want_counts:
-        union_counts = torch.empty(B, k.shape[1], dtype=torch.int32, device=q.device)
+        union_counts = _empty((B, k.shape[1]), torch.int32, q.device, stream)
     return out, mask, counts, union_counts
 
 
@@ -367,10 +377,10 @@ def decode(q, k, v, seq_lens, summ: Summaries, tau, *, block_size: int,
     if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
         raise ValueError("K and V must share shape, strides and dtype")
     out, mask, counts, union_counts = _decode_outputs(q, k, summ, out, mask, counts, union_counts,
-                                                      want_counts)
+                                                      want_counts, stream)
     nbytes = decode_workspace_size(desc, summ.n_blk_cap, p)
     if workspace is None or workspace.numel() < nbytes:
-        workspace = alloc_workspace(nbytes, q.device)
+        workspace = _new_workspace(nbytes, q.device, stream)
     sd = summ.desc()
     _check(load_library().eta_decode(ctypes.byref(desc), _dtype_code(q), _ptr(q), _ptr(k), _ptr(v),
                                      _ptr(seq_lens), ctypes.byref(sd), _ptr(tau), ctypes.byref(p),
@@ -392,10 +402,10 @@ def decode_predicted(q, k, v, seq_lens, summ: Summaries, W, bias, *, block_size:
     if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
         raise ValueError("K and V must share shape, strides and dtype")
     out, mask, counts, union_counts = _decode_outputs(q, k, summ, out, mask, counts, union_counts,
-                                                      want_counts)
+                                                      want_counts, stream)
     nbytes = decode_workspace_size(desc, summ.n_blk_cap, p)
     if workspace is None or workspace.numel() < nbytes:
-        workspace = alloc_workspace(nbytes, q.device)
+        workspace = _new_workspace(nbytes, q.device, stream)
     sd = summ.desc()
     _check(load_library().eta_decode_predicted(
         ctypes.byref(desc), _dtype_code(q), _ptr(q), _ptr(k), _ptr(v), _ptr(seq_lens),
@@ -422,7 +432,7 @@ def decode_predicted_noalloc(q, k, v, seq_lens, summ: Summaries, W, bias, *, blo
     if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
         raise ValueError("K and V must share shape, strides and dtype")
     out, mask, counts, union_counts = _decode_outputs(q, k, summ, out, mask, counts, union_counts,
-                                                      want_counts)
+                                                      want_counts, stream)
     sd = summ.desc()
     _check(load_library().eta_decode_predicted_noalloc(
         ctypes.byref(desc), _dtype_code(q), _ptr(q), _ptr(k), _ptr(v), _ptr(seq_lens),
@@ -446,14 +456,11 @@ class DecodeStep:
         self.params = params if params is not None else decode_params()
         self.desc = kv_desc(k, Hq, block_size)
         self.sdesc = summ.desc()
-        self.out = torch.empty_like(q)
-        self.mask = torch.empty(B, Hq, summ.n_blk_cap, dtype=torch.uint8, device=q.device)
-        self.counts = torch.empty(B, Hq, dtype=torch.int32, device=q.device) if want_counts else None
-        self.union_counts = (torch.empty(B, k.shape[1], dtype=torch.int32, device=q.device)
-                             if want_counts else None)
-        self.tau = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
-        self.workspace = alloc_workspace(decode_workspace_size(self.desc, summ.n_blk_cap, self.params),
-                                         q.device)
+        self.out, self.mask, self.counts, self.union_counts = _decode_outputs(
+            q, k, summ, None, None, None, None, want_counts, stream)
+        self.tau = _empty((B, Hq), torch.float32, q.device, stream)
+        self.workspace = _new_workspace(decode_workspace_size(self.desc, summ.n_blk_cap, self.params),
+                                        q.device, stream)
         self._fn = load_library().eta_decode_predicted
         self._args = (ctypes.byref(self.desc), _dtype_code(q), _ptr(q), _ptr(k), _ptr(v),
                       _ptr(seq_lens), ctypes.byref(self.sdesc), _ptr(W), _ptr(bias),
@@ -473,7 +480,7 @@ def block_bounds(q, seq_lens, summ: Summaries, k_like: torch.Tensor, *, block_si
     B, Hq, d = q.shape
     desc = kv_desc(k_like, Hq, block_size)
     if out is None:
-        out = torch.empty(B, Hq, summ.n_blk_cap, dtype=torch.float32, device=q.device)
+        out = _empty((B, Hq, summ.n_blk_cap), torch.float32, q.device, stream)
     sd = summ.desc()
     _check(load_library().eta_block_bounds(ctypes.byref(desc), _dtype_code(q), _ptr(q),
                                            _ptr(seq_lens), ctypes.byref(sd), ctypes.c_float(z),
@@ -493,10 +500,10 @@ def dense_decode(q, k, v, seq_lens, *, block_size: int = 64, num_splits: int = 0
     B, Hq, d = q.shape
     desc = kv_desc(k, Hq, block_size)
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     nbytes = dense_workspace_size(desc, num_splits)
     if workspace is None or workspace.numel() < nbytes:
-        workspace = alloc_workspace(nbytes, q.device)
+        workspace = _new_workspace(nbytes, q.device, stream)
     _check(load_library().eta_dense_decode(ctypes.byref(desc), _dtype_code(q), _ptr(q), _ptr(k),
                                            _ptr(v), _ptr(seq_lens), _ptr(out), num_splits,
                                            _ptr(workspace), workspace.numel(), _stream(stream)))
@@ -550,8 +557,8 @@ class Calibrator:
 
     def solve(self, stream=None):
         """(c fp32 [Hq], target density fp64 [Hq])."""
-        c = torch.empty(self.Hq, dtype=torch.float32, device=self.hist.device)
-        target = torch.empty(self.Hq, dtype=torch.float64, device=self.hist.device)
+        c = _empty((self.Hq,), torch.float32, self.hist.device, stream)
+        target = _empty((self.Hq,), torch.float64, self.hist.device, stream)
         desc, st = self._desc(1, 1), self._state()
         _check(load_library().eta_calib_solve(ctypes.byref(desc), ctypes.byref(st), _ptr(c),
                                               _ptr(target), _stream(stream)))
@@ -571,11 +578,11 @@ def gated_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: torch.
     assert q.dtype == k.dtype == v.dtype == torch.bfloat16 and tau.dtype == torch.float32
     assert q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and tau.is_contiguous()
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if R is None:
-        R = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
+        R = _empty((B, Hq, T), torch.float32, q.device, stream)
     if L is None:
-        L = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
+        L = _empty((B, Hq, T), torch.float32, q.device, stream)
     desc = PrefillDesc(batch=B, num_q_heads=Hq, num_kv_heads=Hkv, head_dim=d, capacity_tokens=T,
                        dtype=ETA_DT_BF16, beta=beta, additive=int(bool(additive)), C=C)
     _check(load_library().eta_gated_prefill(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v),

@@ -79,8 +79,29 @@ def heads(H, T=5, d=64):
 
 W, LENS = torch.ones(64), torch.ones(2, dtype=I32)
 SCALARS = torch.ones(2, 4, 5)
+Q, KV, TAU = torch.ones(2, 4, 64, dtype=BF), heads(2, T=128), torch.ones(2, 4)
+SUMM = eta.Summaries.empty(2, 2, 64, 2, CPU)
+
+
+def solve(stream):
+    c = eta.Calibrator.__new__(eta.Calibrator)
+    c.Hq, c.Hkv, c.d, c.beta, c.lo, c.hi, c.nb = 4, 2, 64, 4.0, -1.0, 1.0, 8
+    c.hist, c.density = torch.ones(4, 8, dtype=torch.int64), torch.ones(4, dtype=torch.int64)
+    c.solve(stream=stream)
+
 
 CALLS = {
+    "build_block_summaries": lambda s: eta.build_block_summaries(KV, LENS, 64, stream=s),
+    "predict_threshold": lambda s: eta.predict_threshold(Q, None, W[:4], stream=s),
+    "decode": lambda s: eta.decode(Q, KV, KV, LENS, SUMM, TAU, block_size=64, stream=s),
+    "decode_predicted": lambda s: eta.decode_predicted(Q, KV, KV, LENS, SUMM, None, W[:4], block_size=64, stream=s),
+    "decode_predicted_noalloc": lambda s: eta.decode_predicted_noalloc(
+        Q, KV, KV, LENS, SUMM, None, W[:4], block_size=64, stream=s),
+    "DecodeStep": lambda s: eta.DecodeStep(Q, KV, KV, LENS, SUMM, None, W[:4], block_size=64, stream=s).run(),
+    "block_bounds": lambda s: eta.block_bounds(Q, LENS, SUMM, KV, block_size=64, z=1.0, stream=s),
+    "dense_decode": lambda s: eta.dense_decode(Q, KV, KV, LENS, stream=s),
+    "calibrator_solve": solve,
+    "gated_prefill": lambda s: eta.gated_prefill(heads(4), heads(2), heads(2), SCALARS, LENS, beta=4.0, stream=s),
     "qk_norm_rope": lambda s: eta.qk_norm_rope(rows(4), rows(2), rows(2), freqs=None, q_weight=W, stream=s),
     "qk_norm_rope_backward": lambda s: eta.qk_norm_rope_backward(
         heads(4), heads(2), heads(2), rows(4), rows(2), freqs=None, q_weight=W, k_weight=W, stream=s),
