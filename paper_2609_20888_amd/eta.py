@@ -602,6 +602,16 @@ _PLANS: dict = {}
 _PLANS_MOST = 1024
 
 
+def _number(name: str, x) -> float:
+    """A scalar's value now: a plan is found by values, so that a tensor that changes in place
+    (which is hashed by identity) does not find the plan of its former value."""
+    if isinstance(x, torch.Tensor):
+        x = x.item()
+    elif isinstance(x, str):
+        raise TypeError(f"{name} must be a number, got {x!r}")
+    return float(x)
+
+
 def _form(t: Optional[torch.Tensor]):
     return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
@@ -747,6 +757,9 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = N
         rd = _rope_desc(q, k, v, freqs, q_weight, k_weight, eps, interleaved, start, new_lens, k_cache, v_cache)
         _plain("q_out", q_out, (rd.batch, rd.num_q_heads, rd.new_tokens, rd.head_dim), q.dtype)
         return rd, ctypes.byref(rd), dev
+    if type(eps) is not float:
+        eps = _number("eps", eps)
+    interleaved = bool(interleaved)
     rd, ref, dev = _plan((0, eps, interleaved, _form(q), _form(k), _form(v), _form(freqs), _form(q_weight),
                           _form(k_weight), _form(start), _form(new_lens), _form(q_out), _form(k_cache),
                           _form(v_cache)), make)
@@ -794,6 +807,9 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_cache: torch.Tensor,
         n = ctypes.c_size_t()
         _check(load_library().eta_qk_norm_rope_backward_workspace_size(ctypes.byref(rd), ctypes.byref(n)))
         return rd, ctypes.byref(rd), dev, n.value
+    if type(eps) is not float:
+        eps = _number("eps", eps)
+    interleaved = bool(interleaved)
     rd, ref, dev, nbytes = _plan(
         (1, eps, interleaved, _form(q), _form(k), _form(dq_out), _form(dk_cache), _form(dv_cache), _form(freqs),
          _form(q_weight), _form(k_weight), _form(start), _form(new_lens), _form(dq), _form(dk), _form(dv),
@@ -851,6 +867,9 @@ def gated_prefill_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ta
         n = ctypes.c_size_t()
         _check(load_library().eta_gated_prefill_backward_workspace_size(ctypes.byref(pd), ctypes.byref(n)))
         return pd, ctypes.byref(pd), dev, n.value
+    if type(beta) is not float or type(C) is not float:
+        beta, C = _number("beta", beta), _number("C", C)
+    additive = bool(additive)
     pd, ref, dev, nbytes = _plan(
         (2, beta, additive, C, _form(q), _form(k), _form(v), _form(tau), _form(seq_lens), _form(out), _form(L),
          _form(dout), _form(dR), _form(dL), _form(dq), _form(dk), _form(dv), _form(dtau), _form(workspace)), make)
