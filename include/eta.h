@@ -417,6 +417,7 @@ eta_status_t eta_gated_prefill(const eta_prefill_desc_t* pd, const void* q, cons
  * dk and dv over every query head of the kv head's group.  Products on the matrix cores
  * (bf16 operands, fp32 accumulation; P and dS are rounded to bf16 for theirs), everything
  * else fp32; sums in a fixed order (bitwise reproducible).
+ * A beta below 1e-30 counts as 0 in m (and so dtau is 0).
  *   pd          as for the forward; capacity_tokens <= 2^24, and batch * num_q_heads *
  *               capacity_tokens, rounded up to 128 tokens, below 2^30
  *   q, k, v, tau, seq_lens   the forward's inputs

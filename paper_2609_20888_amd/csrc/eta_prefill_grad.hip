@@ -60,7 +60,10 @@ extern "C" __device__ float eta_mul_legacy(float, float) __asm("llvm.amdgcn.fmul
 //   E = kd is2 2^(-beta (S' - tau')) (is2 = 1 / s2),  u = 1 / (E / kd + is2) = s2 sg,  u E = kd (1 - sg),
 //   m / kd = c dS~ + sqrt(d) dR (additive: C dS~ + dR),  s2 sg' m = u (u E) (m / kd).
 // sg' keeps its relative accuracy where the gate is nearly open or nearly shut (the legacy product
-// gives 0 for 0 x inf, the shut gate).
+// gives 0 for 0 x inf, the shut gate).  A beta below kLeastBeta, whose kd would leave E no room in
+// fp32, takes part in the gate alone: kd is kLeastBeta's, dR counts as 0, m (dS~ times 1e-30) is lost in dS~'s
+// rounding, and dtau is 0.
+constexpr float kLeastBeta = 1e-30f;
 struct Gate {
   float s2, is2, nbs, kd, ikd, C, C2, C2is;
   template <int D, bool ADD>
@@ -69,7 +72,7 @@ struct Gate {
     g.s2 = kLog2e / sqrtf((float)D);
     g.is2 = 1.0f / g.s2;
     g.nbs = -beta * g.s2;
-    g.kd = fmaxf(beta, 1e-30f) * (ADD ? 1.0f : 1.0f / sqrtf((float)D));     // (beta 0: m's share is far below any other)
+    g.kd = fmaxf(beta, kLeastBeta) * (ADD ? 1.0f : 1.0f / sqrtf((float)D));
     g.ikd = 1.0f / g.kd;
     g.C = C;
     g.C2 = C * kLog2e;
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(GradArgs a) {
     if (which == 0) v = -a.L[row0 + t] * kLog2e;
     if (which == 1) v = a.beta * kLog2e * a.tau[row0 + t];
     if (which == 2) v = a.dL ? a.dL[row0 + t] - d_s[t] : -d_s[t];
-    if (which == 3) v = a.dR ? a.dR[row0 + t] * (ADD ? 1.0f : sqrtf((float)D)) : 0.f;
+    if (which == 3) v = a.dR && a.beta >= kLeastBeta ? a.dR[row0 + t] * (ADD ? 1.0f : sqrtf((float)D)) : 0.f;
   }
   if (which == 1) {
     const Gate g = Gate::make<D, ADD>(a.beta, a.C);
@@ -428,7 +431,7 @@ __device__ __forceinline__ void grad_q(const GradArgs& a, char* lds, int qblk, i
         const uint32_t hi = in ? pack_bf16x2(acc[db][i + 2] * kLn2, acc[db][i + 3] * kLn2) : 0u;
         *reinterpret_cast<uint2*>(a.dq + (qrow0 + t) * D + 32 * db + 2 * i + 4 * g2) = make_uint2(lo, hi);
       }
-    if (g2 == 0) a.dtau[qrow0 + t] = in && a.beta != 0.f ? -nsum * g.is2 : 0.f;
+    if (g2 == 0) a.dtau[qrow0 + t] = in && a.beta >= kLeastBeta ? -nsum * g.is2 : 0.f;
   }
 }
 
