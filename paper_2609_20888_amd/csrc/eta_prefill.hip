@@ -65,6 +65,22 @@ struct PrefillArgs {
   float beta, C;
 };
 
+// lanes l and l ^ 32 hold the same query row
+__device__ __forceinline__ float row2_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Swizzled 16-byte chunk of (row, chunk) in an unpadded LDS tile of rows of D
+// bf16, XORed by row so that (a) the same chunk of 16 consecutive rows (K reads)
+// and (b) an aligned run of four chunks of four consecutive rows (V transpose
+// reads of 32 dims) both cover all 64 banks once.
+template <int D>
+__device__ __forceinline__ int pf_chunk(int row, int chunk) {
+  if constexpr (D == 128) return chunk ^ (((row & 3) << 2) | ((row >> 2) & 3));
+  return chunk ^ ((((row >> 1) & 1) << 2) | ((row >> 2) & 3));
+}
+
 template <int D, bool ADD>
 __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a) {
   constexpr int KC = D / 16;             // 16-dim chunks (score contraction)
