@@ -31,9 +31,9 @@ namespace {
 // among them) come from a small launch before.
 // What bounds it: vector-ALU issue (three transcendentals and 10 to 12 other instructions for a score of
 // either kind; 84% of the time at d = 64) and at d = 128 the card's power: 16K tokens, 32/8 heads:
-// 8.3 ms, 660 TFLOP/s of the five products and 925 of the seven that run (a plain library product:
+// 8.2 to 8.4 ms, 660 TFLOP/s of the five products and 925 of the seven that run (a plain library product:
 // 1260), the vector unit 69% and the matrix cores 52% busy at 1.85 GHz.  d = 64: 5.3 ms.  4096
-// tokens, 16/4 heads, d = 128: 315 us.
+// tokens, 16/4 heads, d = 128: 306 us (dR and dL given).
 
 constexpr int kGrQ = 128;    // rows (queries or keys) a workgroup owns, 32 per wavefront
 constexpr int kGrT = 64;     // rows of a streamed tile
@@ -224,7 +224,11 @@ __device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32
 }
 
 // A unit's 16 values of a lane, given in order, as the two B operands of a product over the
-// unit's 32 rows (bf16 pairs).
+// unit's 32 rows (bf16 pairs).  P and dS are rounded to bf16 here, once, for the products into dv, dq and dk (the
+// sums stay fp32): the matrix cores take both operands in one type, and K, Q and dO are bf16.  In fp32
+// these three products would run at a sixteenth of the bf16 rate; as two bf16 parts, high and low, they would be
+// six.  It costs a half step of each term, which average: relative 2-norms of the results against 64 bits
+// 2.3e-3 to 2.4e-3, with fp32 P and dS 1.7e-3, the rounding of the results alone.  dtau takes neither.
 struct Packer {
   u32x4 o[2];
   float hold;

@@ -19,18 +19,14 @@ namespace {
 // 2^19 an fp32 angle is off by up to 2^-6 radians), its fraction in fp32.
 //
 // What bounds it: memory, each row read once and written once (16K tokens, 32/8 heads, d = 128, bf16:
-// 81 us, 5.0 TB/s, where a device copy reaches 5.2; the gradients 116 us, 4.9 TB/s).  A lane holds 16 bytes
+// 82 us, 4.9 TB/s, where a device copy reaches 5.2; the gradients 116 us, 4.9 TB/s).  A lane holds 16 bytes
 // of a row, so a row of 256 bytes is 16 lanes and its sum of squares four DPP steps; the
 // lanes of a row keep one token and walk over heads, so that sines, cosines and weights
 // stay in registers (16 heads a workgroup: 90 us before the hints below, 8: 95, 4: 116).
 
 // 16 bytes of a row, read once: with the non-temporal hint (16K tokens, 32/8 heads, d = 128, bf16,
-// backward: 125 -> 108 us; 4 x 2000, 32/4, d = 64, fp32: 46.5 -> 42.6 us).  The forward writes with it
-// too (STREAM) where the call's bytes pass what the last-level cache holds beside other work: 246 MB
-// 56 -> 52 us, 403 MB 88 -> 81 us; at 202 MB the two are equal, and below that what is written is
-// best left in the cache for its reader (fp32, 147 MB: 28 us, with the hint 30).  The backward, which
-// writes a third of its bytes, does so from further on: 570 MB 126 -> 116 us where each call has other
-// result buffers; 188 MB 46 us, with the hint 52.
+// backward into the same results each time: 125 -> 108 us; 4 x 2000, 32/4, d = 64, fp32: 46.5 -> 42.6 us).
+// With STREAM the results are written with it too (plan_rope has the rule and what it measured).
 typedef uint32_t u32x4n __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 get16(const char* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(p)));

@@ -20,7 +20,7 @@ struct RopePlan {
   int heads;                 // heads of a workgroup
   int nq, nk, nv;            // workgroups along the heads of q, k and v
   int steps;                 // gradients: workgroups along the tiles (each takes every steps-th)
-  bool stream;               // results written past the caches
+  bool stream;               // results written past the caches (plan_rope)
 };
 RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad);
 

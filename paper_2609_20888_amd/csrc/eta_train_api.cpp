@@ -122,6 +122,15 @@ size_t rope_grad_bytes(const eta_rope_desc_t& rd, const RopePlan& p) {
 // A workgroup takes as many heads as still leave about four workgroups per compute unit
 // (sines and weights are formed once for them), at most 16 (32: 94 us against 90 at 16K tokens).  Gradients: the workgroups along
 // the tiles are limited by the rows of partial weight gradients.
+//
+// Results are written past the caches where the bytes of the call (rows read and written; bf16, 32/8 heads,
+// d = 128) leave the last-level cache too little for their reader.  Forward, from 200 MiB on: 192 MiB
+// 44.2 us with the caches, 45.1 past them; 211: 50.4, 49.2; 234: 54.8, 52.5; 384: 86.3, 82.3.  The gradients,
+// which write a third of their bytes, alone gain from 230 MiB on (239 MiB 57.4, 56.2; 457: 103, 94), but
+// with a reader of dq behind them only from about 400 (288 MiB: 86.6 with the caches, 88.0 past them; 352:
+// 102.8, 103.6; 404: 118, 115; 457: 132, 128; 576: 168, 158; fp32, d = 64, 469 MiB: 137 both), and not at
+// all where every call writes the same buffers, as a replayed graph does (457 MiB: 117, 127; 576: 150, 158).
+// 480 MiB lies where new buffers gain more than same ones lose.
 RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad) {
   RopePlan p{};
   p.tile = 256 / (rd.head_dim * elem_bytes(rd.dtype) / 16);
@@ -140,9 +149,12 @@ RopePlan plan_rope(const eta_rope_desc_t& rd, bool has_v, bool grad) {
 }
 
 // The heads of a group are split while the workgroups of 128 keys do not fill two per compute unit: the
-// longest walk of a workgroup is otherwise the call's time (4096 tokens, 16/4 heads, d = 128: 698 us whole,
-// 422 split in two, 336 in four; 2 x 2048: 349, 212, 174).  From there on the partials cost more than the
-// walks gain (8192 tokens: 1122 us in two, 1218 in four; 4 x 2000, 32/4, d = 64: 440, 466).
+// longest walk of a workgroup is otherwise the call's time (4096 tokens, 16/4 heads, d = 128: 392 us split
+// in two, 317 in four; 2 x 2048: 208, 174; 8192: 1486 whole, 1041 in two; 4 x 2000, 32/4, d = 64: 493,
+// 381).  From there on the partials cost what the walks gain (8192 tokens: 1041 us in two, 1053 in four; 4 x
+// 2000, 32/4: d = 64 381, 390, d = 128 584, 617).  Workgroups are counted by the capacity, the lengths being on
+// the device; the same batch with lengths 2000, 1073, 1646 and 719: d = 64 276 in two, 261 in four, d = 128
+// 389, 393.
 GradPlan plan_prefill_grad(const eta_prefill_desc_t& pd) {
   GradPlan p;
   p.blocks = (pd.capacity_tokens + 127) / 128;
