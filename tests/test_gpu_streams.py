@@ -141,3 +141,27 @@ def test_two_streams_at_once():
     for g, w in zip(got, want):
         for a, b in zip(g, w):
             assert torch.equal(a, b)
+
+
+def test_captured_on_a_side_stream():
+    """A gradient call on a side stream inside a capture: replayed on other inputs with eager calls, and
+    buffers taken and given back, between the replays."""
+    q, k, v, tau, lens, dout = prefill_inputs()
+    out, _, L = eta.gated_prefill(q, k, v, tau, lens, beta=4.0)
+    douts = [dout.clone(), (-0.5 * dout).contiguous(), dout.flip(2).contiguous()]
+    want = [eta.gated_prefill_backward(q, k, v, tau, lens, out, L, x, beta=4.0) for x in douts]
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = eta.gated_prefill_backward(q, k, v, tau, lens, out, L, dout, beta=4.0, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for x, w in zip(douts, want):
+            dout.copy_(x)
+            for n in range(8, 25):
+                torch.empty(1 << n, dtype=torch.uint8, device="cuda").fill_(255)
+            graph.replay()
+            for a, b in zip(got, w):
+                assert torch.equal(a, b)
+            eta.gated_prefill_backward(q, k, v, tau, lens, out, L, douts[1], beta=4.0, stream=side)
