@@ -542,6 +542,184 @@ eta_status_t eta_dense_decode(const eta_kv_desc_t* kv, int32_t q_dtype, const vo
                               int32_t num_splits, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/*
+ * Paged 8-bit cache.  A page holds one block of b = block_size tokens of every kv head:
+ * keys and values as 8-bit E4M3 codes (bias 7, 3 fraction bits, largest finite 448) with one
+ * fp32 scale for each page and kv head; a value is its code times that scale.  Keys lie by
+ * token, values by dimension (the sums over tokens of p.V then run along contiguous bytes):
+ *   k[p*page_stride + (h*b + t)*d + i],  v[p*page_stride + (h*d + i)*b + t]
+ *   k_scale[p*scale_stride + h],  v_scale alike
+ * for page p < num_pages, kv head h, token t < b of the page, dimension i < d = head_dim.
+ * Row x of the page table lists the pages of sequence x: block j (tokens [j*b, (j+1)*b)) is
+ * page table[x*table_stride + j], j < table_blocks.  An entry outside [0, num_pages) names no
+ * page: rows are not stored there, no record is written for it, and its tokens are attended
+ * by no head.  A page may be in several rows; what is stored into it, all of them read.
+ * Lengths are clamped to [0, table_blocks*b].
+ */
+typedef struct {
+  int32_t batch;               /* rows of the table; <= 65535 */
+  int32_t num_q_heads;         /* <= 256 */
+  int32_t num_kv_heads;        /* num_q_heads / num_kv_heads in {1, 2, 4, 8} */
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t block_size;          /* 64 or 128 */
+  int32_t reserved;            /* 0 */
+  int64_t num_pages;           /* >= 1, < 2^31 */
+  int64_t table_blocks;        /* >= 1; table_blocks * block_size < 2^31 */
+  int64_t table_stride;        /* elements, >= table_blocks (batch 1: any) */
+  int64_t page_stride;         /* codes, a multiple of 16, >= num_kv_heads*block_size*head_dim */
+  int64_t scale_stride;        /* elements, >= num_kv_heads */
+} eta_page_desc_t;
+
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+} eta_page_pool_t;
+
+/* New keys and values: element (b, h, i, c) of k at k[b*k_stride_b + h*k_stride_h + i*k_stride_t + c]
+ * for new token i < new_tokens (strides in elements, >= 0, rows of head_dim contiguous and
+ * 16-byte aligned), v alike. */
+typedef struct {
+  const void* k;
+  const void* v;
+  int32_t new_tokens;          /* >= 1 */
+  int32_t dtype;               /* ETA_DT_F32 or ETA_DT_BF16 */
+  int64_t k_stride_b, k_stride_h, k_stride_t;
+  int64_t v_stride_b, v_stride_h, v_stride_t;
+} eta_page_rows_t;
+
+/*
+ * eta_page_store -- rounds new tokens into the pages: token i < new_lens[x] of sequence x is
+ * stored at position start[x] + i (positions past the table, or on an entry that names no page:
+ * not stored).  For each page and head that new tokens fall into, with the page's tokens before
+ * the first of them as the ones it holds already:
+ *   scale = the least power of two s (2^-126 at least) with |x| <= 448 s for every finite new x,
+ *           and no less than the page's present scale where it holds tokens already;
+ *   new codes = x / scale to the nearest, ties to even; NaN and infinities become NaN;
+ *   where the scale grows, the codes of the tokens held are rounded once more, to
+ *   code * (old scale / scale) (exact for powers of two but below 2^-6 of the new scale).
+ * Codes of the page's tokens behind the new ones are left as they were: the newest token ends
+ * its sequence.  So a cache filled token by token and one filled in chunks have the same scales,
+ * and the same codes wherever no code fell below 2^-6 on the way.
+ *   start, new_lens  device int32 [batch], or NULL: 0, new_tokens (start below 0 counts as 0,
+ *                    new_lens are clamped to [0, new_tokens])
+ * No two tokens of one call may fall into the same page by different rows of the table.
+ */
+eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* table,
+                            const eta_page_rows_t* rows, const int32_t* start, const int32_t* new_lens,
+                            void* stream);
+
+/*
+ * eta_page_summaries -- the block index of the keys as the pages hold them: mu, sigma and M (see
+ * eta_build_block_summaries; flat sigma) of every full block, or, with prev_lens, of blocks
+ * prev_lens[b] / b .. + max_new_blocks - 1 that are full (see eta_update_block_summaries).
+ * Blocks past n_blk_cap, and those without a page, are not written.
+ */
+eta_status_t eta_page_summaries(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* table,
+                                const int32_t* prev_lens, const int32_t* seq_lens, int32_t max_new_blocks,
+                                const eta_summary_t* out, void* stream);
+
+/*
+ * eta_page_decode, eta_page_decode_predicted -- eta_decode and eta_decode_predicted over the
+ * pages: the same screening, thresholds, rescue, results and parameters, K and V being what the
+ * pages hold.  Lengths are clamped to [0, min(table_blocks*b, n_blk_cap*b + b - 1)], so the
+ * index may leave out a last block that is never full.  Products on the matrix cores from
+ * operands that hold the codes and bf16 queries exactly (fp32 queries in three bf16 parts) and
+ * the softmax weights in two (three) bf16 parts; sums and statistics in fp32.
+ *   workspace   >= eta_page_decode_workspace_size() bytes, 256-byte aligned
+ */
+eta_status_t eta_page_decode_workspace_size(const eta_page_desc_t* pd, int64_t n_blk_cap,
+                                            const eta_decode_params_t* p, size_t* bytes);
+eta_status_t eta_page_decode(const eta_page_desc_t* pd, int32_t q_dtype, const void* q,
+                             const eta_page_pool_t* pool, const int32_t* table, const int32_t* seq_lens,
+                             const eta_summary_t* summ, const float* tau, const eta_decode_params_t* p,
+                             void* out, uint8_t* block_mask, int32_t* head_token_counts,
+                             int32_t* union_counts, void* workspace, size_t workspace_bytes, void* stream);
+eta_status_t eta_page_decode_predicted(const eta_page_desc_t* pd, int32_t q_dtype, const void* q,
+                                       const eta_page_pool_t* pool, const int32_t* table,
+                                       const int32_t* seq_lens, const eta_summary_t* summ, const float* W,
+                                       const float* bias, const eta_decode_params_t* p, void* out,
+                                       uint8_t* block_mask, int32_t* head_token_counts,
+                                       int32_t* union_counts, float* tau_out, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* eta_page_dense_decode -- eta_dense_decode over the pages (every token that has a page). */
+eta_status_t eta_page_dense_workspace_size(const eta_page_desc_t* pd, int32_t num_splits, size_t* bytes);
+eta_status_t eta_page_dense_decode(const eta_page_desc_t* pd, int32_t q_dtype, const void* q,
+                                   const eta_page_pool_t* pool, const int32_t* table,
+                                   const int32_t* seq_lens, void* out, int32_t num_splits, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * Page tables.  refs[p] counts the holders of page p, each table entry that names it and whatever
+ * else the caller counts (a list of shared beginnings); a page is free when refs[p] <= 0.  One
+ * table serves the caches of all layers: these calls change tables and counts alone, and say
+ * which pages have to be copied (src -> dst); eta_page_copy does that for one layer's pool.
+ * New pages are the free ones of the lowest numbers, given to the rows in order.
+ */
+typedef struct {
+  int32_t batch;               /* rows, <= 65535 */
+  int32_t block_size;          /* tokens of a page, >= 1 */
+  int64_t num_pages;           /* < 2^31 */
+  int64_t table_blocks;        /* entries of a row, >= 1; table_blocks * block_size < 2^31 */
+  int64_t table_stride;        /* elements between rows of every table of the call, >= table_blocks */
+} eta_table_desc_t;
+
+/* Bytes of workspace that each of the three calls below needs. */
+eta_status_t eta_page_table_workspace_size(const eta_table_desc_t* td, size_t* bytes);
+
+/*
+ * eta_page_extend -- gives a page to every block that has tokens (j < ceil(seq_lens[b] /
+ * block_size), lengths clamped to the table) and whose entry is negative, and counts it in refs.
+ *   table, refs  changed in place
+ *   missing      int32 [1]: how many blocks found no free page (their entries stay as they are)
+ */
+eta_status_t eta_page_extend(const eta_table_desc_t* td, int32_t* table, int32_t* refs,
+                             const int32_t* seq_lens, int32_t* missing, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * eta_page_fork -- every row goes on from a row of the table as it was: row b takes the first
+ * blocks of row a = parents[b] that have tokens and its length; a outside [0, batch) leaves the
+ * row empty.  Full blocks are shared.  A last block that is not full goes to the first row that
+ * takes it; each further one gets a page of its own and a copy to make.  Entries behind a row's
+ * last block, and those of an empty row, are -1.  refs gains the new table's entries and loses
+ * the old one's, so the pages that no row goes on with become free (and may be given out again
+ * by the same call).
+ *   table, refs, seq_lens         as they were;  table_out, refs_out, seq_lens_out: the new ones
+ *   src, dst  int32 [batch]: for each row the page to copy and its own new one, or -1, -1
+ *   missing   int32 [1]: how many rows found no free page (their last block's entry is -1)
+ * No output may overlap an input or another output.
+ */
+eta_status_t eta_page_fork(const eta_table_desc_t* td, const int32_t* table, const int32_t* refs,
+                           const int32_t* seq_lens, const int32_t* parents, int32_t* table_out,
+                           int32_t* refs_out, int32_t* seq_lens_out, int32_t* src, int32_t* dst,
+                           int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * eta_page_compact -- renumbers the pages so that the ones in use are the first: with n of them,
+ * the k-th page in use from number n on takes the number of the k-th free one below n; the
+ * others stay.  Entries that name a free page, or none, become -1; refs move with their pages
+ * (free ones: 0).
+ *   src, dst  int32 [num_pages / 2]: the pages to copy, in order, then -1, -1
+ *   live      int32 [1]: n
+ * No output may overlap an input or another output.  src and dst may be NULL when num_pages is 1.
+ */
+eta_status_t eta_page_compact(const eta_table_desc_t* td, const int32_t* table, const int32_t* refs,
+                              int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst,
+                              int32_t* live, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * eta_page_copy -- copies page src[i] of the pool (codes and scales of every head) over page
+ * dst[i], i < n.  Pairs with a number outside [0, num_pages) are passed over.  A page may be
+ * copied to several, but no page may be both copied and written, or written twice
+ * (eta_page_fork and eta_page_compact name none such).  Of the descriptor the heads, sizes,
+ * num_pages and the pool's strides are read.
+ */
+eta_status_t eta_page_copy(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* src,
+                           const int32_t* dst, int64_t n, void* stream);
+
 /* Human-readable detail of the last failure on this host thread ("" if none). */
 const char* eta_last_error_string(void);
 
@@ -577,7 +755,13 @@ typedef enum {
   ETA_KERNEL_PREFILL_GRAD_ROWS = 14,
   ETA_KERNEL_PREFILL_GRAD = 15,
   ETA_KERNEL_PREFILL_GRAD_JOIN = 16,
-  ETA_KERNEL_ALL_KINDS = 17
+  ETA_KERNEL_PAGE_STORE = 17,
+  ETA_KERNEL_PAGE_SUMMARIES = 18,
+  ETA_KERNEL_PAGE_SPLIT = 19,
+  ETA_KERNEL_PAGE_DENSE_SPLIT = 20,
+  ETA_KERNEL_PAGE_TABLE = 21,
+  ETA_KERNEL_PAGE_COPY = 22,
+  ETA_KERNEL_ALL_KINDS = 23
 } eta_kernel_kind_t;
 
 typedef struct {

@@ -22,7 +22,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libeta.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("eta_kernels.hip", "eta_prefill.hip", "eta_api.cpp",
                                            "eta_prefill_grad.hip", "eta_rope.hip",
-                                           "eta_train_api.cpp")]
+                                           "eta_train_api.cpp", "eta_page.hip",
+                                           "eta_page_attend.hip", "eta_page_api.cpp")]
 # (source, extra flags, object name): eta_kernels.hip holds split decode on bf16
 # caches in part 1, on fp32 caches in part 2, and everything else in part 0
 UNITS = [(SOURCES[0], [f"-DETA_PART={p}"], f"eta_kernels.{p}.o") for p in (0, 1, 2)] + \

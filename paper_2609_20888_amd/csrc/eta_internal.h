@@ -102,6 +102,18 @@ hipError_t launch_decode(const Geom& g, const DecodeCfg& c, int q_dtype, const v
                          int32_t* counts, int32_t* union_counts, const DecodeWs& ws,
                          hipStream_t stream, LaunchHook hook);
 
+// The parts of launch_decode and launch_dense that do not read the cache: the thresholds and the
+// screening before it, and the merge of the splits' partials behind it.
+hipError_t launch_screen(const Geom& g, const DecodeCfg& c, int q_dtype, const void* q,
+                         const int32_t* seq_lens, const eta_summary_t& s, const float* tau,
+                         const float* W, const float* bias, float* tau_out, uint8_t* mask,
+                         const DecodeWs& ws, hipStream_t stream, LaunchHook hook);
+hipError_t launch_combine(const Geom& g, const SplitPlan& plan, int q_dtype, const int32_t* seq_lens,
+                          void* out, int32_t* counts, int32_t* union_counts, const DecodeWs& ws,
+                          hipStream_t stream, LaunchHook hook);
+hipError_t launch_dense_combine(const Geom& g, int S, int q_dtype, const int32_t* seq_lens, void* out,
+                                const DecodeWs& ws, hipStream_t stream, LaunchHook hook);
+
 hipError_t launch_bounds(const Geom& g, int q_dtype, const void* q, const int32_t* seq_lens,
                          const eta_summary_t& s, float z, float* bounds, hipStream_t stream,
                          LaunchHook hook);

@@ -31,6 +31,7 @@
 #include "eta_device.h"
 #include "eta_index.h"
 #include "eta_internal.h"
+#include "eta_lanes.h"
 
 // The source compiles to three objects, in parallel (ETA_PART): 0 holds every
 // kernel but split decode, and the host launchers; 1 and 2 hold split decode
@@ -223,23 +224,6 @@ __device__ __forceinline__ float wave_max(float x) {
 }
 __device__ __forceinline__ float wave_sum(float x) {
   return wave_reduce(x, [](float a, float b) { return a + b; });
-}
-
-// Inclusive prefix sum of an integer over the wavefront's lanes, on the vector
-// ALUs: shifts by 1, 2, 4 and 8 lanes within each 16-lane row (a lane whose
-// source would lie in the previous row adds 0), then each row adds the totals
-// of the rows before it, read from lanes 15, 31 and 47.  Lane 63 ends with the
-// wavefront's total.  Full EXEC only.
-__device__ __forceinline__ int wave_incl_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
-  const int r0 = __builtin_amdgcn_readlane(x, 15);
-  const int r1 = r0 + __builtin_amdgcn_readlane(x, 31);
-  const int r2 = r1 + __builtin_amdgcn_readlane(x, 47);
-  const int row = (int)(threadIdx.x & 63) >> 4;
-  return x + (row == 0 ? 0 : (row == 1 ? r0 : (row == 2 ? r1 : r2)));
 }
 
 // ---------------------------------------------------------------- summaries
@@ -2513,12 +2497,10 @@ void launch_combine_impl(const Geom& g, const CombineArgs& ca, hipStream_t strea
 // L2 bytes of W that the fused predictor may re-read per step (see launch_decode)
 constexpr int64_t kFusedPredictMaxBytes = 64ll << 20;
 
-hipError_t launch_decode(const Geom& g, const DecodeCfg& c, int q_dtype, const void* q,
-                         const void* k, const void* v, const int32_t* seq_lens,
-                         const eta_summary_t& s, const float* tau, const float* W,
-                         const float* bias, float* tau_out, void* out, uint8_t* mask,
-                         int32_t* counts, int32_t* union_counts, const DecodeWs& ws,
-                         hipStream_t stream, LaunchHook hook) {
+hipError_t launch_screen(const Geom& g, const DecodeCfg& c, int q_dtype, const void* q,
+                         const int32_t* seq_lens, const eta_summary_t& s, const float* tau,
+                         const float* W, const float* bias, float* tau_out, uint8_t* mask,
+                         const DecodeWs& ws, hipStream_t stream, LaunchHook hook) {
   const bool predict = tau == nullptr;
   // The fused predictor reads its group's G rows of W in every screening
   // workgroup: B Hkv n_tiles Hq D G 4 bytes of L2 reads per step.  Past
@@ -2535,10 +2517,36 @@ hipError_t launch_decode(const Geom& g, const DecodeCfg& c, int q_dtype, const v
                 s.max_norm, mask, ws.ids, ws.tile_cnt, ws.head_cnt, nullptr, ws.resc_best,
                 ws.resc_info, ws.wbits, g, q_dtype, (predict && !separate) ? 1 : 0, c.z,
                 c.offset_a, c.rescue_window, c.lwb, c.screen_all};
-  hipError_t e = with_hook(hook, ETA_KERNEL_SCREEN, stream,
-                           [&] { launch_screen_impl<false>(g, sa, stream); });
+  return with_hook(hook, ETA_KERNEL_SCREEN, stream,
+                   [&] { launch_screen_impl<false>(g, sa, stream); });
+}
+
+hipError_t launch_combine(const Geom& g, const SplitPlan& plan, int q_dtype, const int32_t* seq_lens,
+                          void* out, int32_t* counts, int32_t* union_counts, const DecodeWs& ws,
+                          hipStream_t stream, LaunchHook hook) {
+  CombineArgs ca{ws.part_ml, ws.part_acc, ws.head_cnt, ws.tile_cnt, seq_lens, ws.resc_out,
+                 ws.extra_union, plan.S > 0 ? nullptr : ws.plan, counts, union_counts, out, g,
+                 q_dtype, plan.S};
+  return with_hook(hook, ETA_KERNEL_COMBINE, stream, [&] { launch_combine_impl(g, ca, stream); });
+}
+
+hipError_t launch_dense_combine(const Geom& g, int S, int q_dtype, const int32_t* seq_lens, void* out,
+                                const DecodeWs& ws, hipStream_t stream, LaunchHook hook) {
+  CombineArgs ca{ws.part_ml, ws.part_acc, nullptr, nullptr, seq_lens, nullptr, nullptr,
+                 S > 0 ? nullptr : ws.plan, nullptr, nullptr, out, g, q_dtype, S};
+  return with_hook(hook, ETA_KERNEL_DENSE_COMBINE, stream,
+                   [&] { launch_combine_impl(g, ca, stream); });
+}
+
+hipError_t launch_decode(const Geom& g, const DecodeCfg& c, int q_dtype, const void* q,
+                         const void* k, const void* v, const int32_t* seq_lens,
+                         const eta_summary_t& s, const float* tau, const float* W,
+                         const float* bias, float* tau_out, void* out, uint8_t* mask,
+                         int32_t* counts, int32_t* union_counts, const DecodeWs& ws,
+                         hipStream_t stream, LaunchHook hook) {
+  hipError_t e = launch_screen(g, c, q_dtype, q, seq_lens, s, tau, W, bias, tau_out, mask, ws, stream, hook);
   if (e != hipSuccess) return e;
-  SplitArgs sp{q, k, v, seq_lens, predict ? ws.tau : tau, ws.ids, ws.tile_cnt, ws.part_ml,
+  SplitArgs sp{q, k, v, seq_lens, tau == nullptr ? ws.tau : tau, ws.ids, ws.tile_cnt, ws.part_ml,
                ws.part_acc, ws.resc_best, ws.resc_info, ws.wbits, mask, ws.resc_out,
                ws.extra_union, ws.plan, ws.head_cnt, out, counts, union_counts, g, q_dtype,
                c.beta, c.offset_a, c.self_ungated, c.rescue_window};
@@ -2546,10 +2554,7 @@ hipError_t launch_decode(const Geom& g, const DecodeCfg& c, int q_dtype, const v
                 [&] { launch_split_impl<false>(g, c.plan, sp, stream); });
   if (e != hipSuccess) return e;
   if (c.plan.S == 1) return hipSuccess;     // one split per group wrote the results
-  CombineArgs ca{ws.part_ml, ws.part_acc, ws.head_cnt, ws.tile_cnt, seq_lens, ws.resc_out,
-                 ws.extra_union, c.plan.S > 0 ? nullptr : ws.plan, counts, union_counts, out, g,
-                 q_dtype, c.plan.S};
-  return with_hook(hook, ETA_KERNEL_COMBINE, stream, [&] { launch_combine_impl(g, ca, stream); });
+  return launch_combine(g, c.plan, q_dtype, seq_lens, out, counts, union_counts, ws, stream, hook);
 }
 
 hipError_t launch_bounds(const Geom& g, int q_dtype, const void* q, const int32_t* seq_lens,
@@ -2599,10 +2604,7 @@ hipError_t launch_dense(const Geom& g, int S, int q_dtype, const void* q, const 
   hipError_t e = with_hook(hook, ETA_KERNEL_DENSE_SPLIT, stream,
                            [&] { launch_split_impl<true>(g, plan, sp, stream); });
   if (e != hipSuccess || S == 1) return e;     // one split per group wrote the output
-  CombineArgs ca{ws.part_ml, ws.part_acc, nullptr, nullptr, seq_lens, nullptr, nullptr,
-                 S > 0 ? nullptr : ws.plan, nullptr, nullptr, out, g, q_dtype, S};
-  return with_hook(hook, ETA_KERNEL_DENSE_COMBINE, stream,
-                   [&] { launch_combine_impl(g, ca, stream); });
+  return launch_dense_combine(g, S, q_dtype, seq_lens, out, ws, stream, hook);
 }
 
 // ---------------------------------------------------------------- library scratch

@@ -1,0 +1,682 @@
+// The paged 8-bit cache but for its attention (gfx950): storing, the index, copies, tables.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "eta_device.h"
+#include "eta_lanes.h"
+#include "eta_page.h"
+
+namespace eta {
+namespace {
+
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------- storing
+//
+// A page's scale is a power of two, so that a page whose scale grows, as tokens come one by one,
+// keeps its codes' values: E4M3 has as many fraction bits at every exponent, so only codes that
+// fall below 2^-6 of the new scale are rounded again, and x / scale is exact.  (A scale of
+// amax / 448 would round every code again at each growth, for less than one bit of range.)
+
+// Exponent e of the least 2^e with amax <= 448 * 2^e (448 = 1.75 * 2^8), at least -126.
+__device__ __forceinline__ int scale_exponent(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e < -126 ? -126 : e;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// |x|, or 0 where x is NaN or infinite
+__device__ __forceinline__ float finite_abs(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+  return u < 0x7f800000u ? __uint_as_float(u) : 0.f;
+}
+
+// x / scale as it is coded: infinities become NaN (the conversion rounds to nearest, ties to
+// even, and |x| / scale never passes 448)
+__device__ __forceinline__ float coded(float x, float inv) {
+  return (__float_as_uint(x) & 0x7fffffffu) == 0x7f800000u ? __builtin_nanf("") : x * inv;
+}
+
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// the codes of a word times r, rounded again
+__device__ __forceinline__ uint32_t scaled4(uint32_t w, float r) {
+  const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return pack4(lo[0] * r, lo[1] * r, hi[0] * r, hi[1] * r);
+}
+
+// Eight elements of a row in 32 bits.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+}
+
+struct StoreArgs {
+  uint8_t* code[2];              // k, v
+  float* scale[2];
+  const void* rows[2];
+  int64_t sb[2], sh[2], st[2];
+  const int32_t* table;
+  const int32_t* start;
+  const int32_t* new_lens;
+  PageGeom pg;
+  int new_tokens;
+};
+
+// New tokens [first, end) of a sequence, in positions.
+__device__ __forceinline__ void new_span(const StoreArgs& a, int b, int64_t* first, int64_t* end) {
+  int64_t s = a.start != nullptr ? a.start[b] : 0;
+  int64_t n = a.new_lens != nullptr ? a.new_lens[b] : a.new_tokens;
+  s = s < 0 ? 0 : s;
+  n = n < 0 ? 0 : (n > a.new_tokens ? a.new_tokens : n);
+  *first = s;
+  *end = s + n;
+}
+
+// One workgroup for a page and head of K or of V (blockIdx.x even, odd).  A thread holds 8 dims
+// of 4 consecutive tokens, so that V's transposed codes form whole words of 4 tokens, which go
+// through LDS to rows of the page.
+template <int D, int BS, typename T>
+__global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs a) {
+  constexpr int TPR = D / 8, NT = TPR * (BS / 4), NW = NT / 64;
+  __shared__ float red_s[NW];
+  __shared__ uint32_t v_s[D][BS / 4 + 1];
+  const int kv = blockIdx.x & 1, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int c = tid % TPR, q4 = tid / TPR;            // dims 8 c .., tokens 4 q4 .. of the page
+  int64_t first, end;
+  new_span(a, b, &first, &end);
+  const int64_t j = first / BS + (blockIdx.x >> 1), base = j * BS;
+  const int64_t lo64 = first > base ? first - base : 0, hi64 = end - base < BS ? end - base : BS;
+  if (hi64 <= lo64) return;
+  const int lo = (int)lo64, hi = (int)hi64;
+  const int64_t page = page_of(a.table + (int64_t)b * a.pg.table_stride, j, a.pg.table_blocks, a.pg.pages);
+  if (page < 0) return;
+  const int64_t si = page * a.pg.scale_stride + h;
+  const float held = a.scale[kv][si];
+  const T* src = reinterpret_cast<const T*>(a.rows[kv]) + b * a.sb[kv] + h * a.sh[kv];
+  uint8_t* dst = a.code[kv] + page * a.pg.page_stride + (int64_t)h * BS * D;
+  float x[4][8], amax = 0.f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int t = 4 * q4 + r;
+    const int64_t i = (t >= lo && t < hi ? t : lo) + base - first;      // (others read a new row too)
+    load8<T>(src + i * a.st[kv] + 8 * c, x[r]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_abs(x[r][e]));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
+  if ((tid & 63) == 0) red_s[tid >> 6] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < NW; ++k) amax = fmaxf(amax, red_s[k]);
+  const int e2 = scale_exponent(amax);
+  const float need = power_of_two(e2);
+  // (a scale held that is no power of two, or NaN, is kept where it is not less)
+  const bool grows = lo == 0 || need > held;
+  const float scale = grows ? need : held;
+  const float inv = grows ? power_of_two(-e2) : 1.0f / held, again = held / scale;
+  const bool round_held = lo > 0 && grows;
+  if (tid == 0 && grows) a.scale[kv][si] = scale;
+  if (kv == 0) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = 4 * q4 + r;
+      uint2* p = reinterpret_cast<uint2*>(dst + t * D + 8 * c);
+      if (t >= lo && t < hi) {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = coded(x[r][e], inv);
+        *p = make_uint2(pack4(y[0], y[1], y[2], y[3]), pack4(y[4], y[5], y[6], y[7]));
+      } else if (t < lo && round_held) {
+        const uint2 w = *p;
+        *p = make_uint2(scaled4(w.x, again), scaled4(w.y, again));
+      }
+    }
+    return;
+  }
+  const int t0 = 4 * q4;
+  const bool whole = t0 >= lo && t0 + 4 <= hi;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t w = pack4(coded(x[0][e], inv), coded(x[1][e], inv), coded(x[2][e], inv), coded(x[3][e], inv));
+    if (!whole) {
+      const uint32_t old = *reinterpret_cast<const uint32_t*>(dst + (8 * c + e) * BS + t0);
+      const uint32_t rounded = round_held ? scaled4(old, again) : old;
+      uint32_t m = 0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const uint32_t byte = 0xffu << (8 * r);
+        m |= (t0 + r < lo ? rounded : (t0 + r < hi ? w : old)) & byte;
+      }
+      w = m;
+    }
+    v_s[8 * c + e][q4] = w;
+  }
+  __syncthreads();
+  constexpr int WPR = BS / 16;                        // 16-byte pieces of a row of V
+  for (int k = tid; k < D * WPR; k += NT) {
+    const int d = k / WPR, p = k % WPR;
+    const uint32_t* s = &v_s[d][4 * p];
+    *reinterpret_cast<uint4*>(dst + d * BS + 16 * p) = make_uint4(s[0], s[1], s[2], s[3]);
+  }
+}
+
+// ---------------------------------------------------------------- the index
+//
+// Wavefront w of a workgroup takes blocks w, w + 4, .. of its NB: a load covers whole rows (LPR
+// lanes of 16 codes), the block stays in registers for both passes (mean, then the mean squared
+// deviation from it), the rows' norms are summed over a row's lanes.  Sums run on the codes; the
+// page's scale is applied once.  Results leave as rows of the dimension-major records.
+
+// the sum (or maximum) over lanes l, l ^ N, l ^ 2 N, .. in every lane
+template <int N, typename Op>
+__device__ __forceinline__ float over_rows(float x, Op op) {
+#pragma unroll
+  for (int o = N; o < 64; o <<= 1) x = op(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+__device__ __forceinline__ uint8_t to_record8(float f) {     // saturating at 448, NaN stays
+  const float a = fabsf(f) > 448.0f ? copysignf(448.0f, f) : f;
+  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, a, 0, false);
+}
+
+struct IndexArgs {
+  const uint8_t* k;
+  const float* k_scale;
+  const int32_t* table;
+  const int32_t* prev_lens;
+  const int32_t* seq_lens;
+  void* mu;
+  void* sigma;
+  float* mx;
+  PageGeom pg;
+  int max_new;
+};
+
+template <int D, int BS, int NB>
+__global__ __launch_bounds__(256) void page_summaries_kernel(IndexArgs a) {
+  constexpr int LPR = D / 16, R = 64 / LPR, NI = BS / R;
+  __shared__ float mu_s[D][NB + 1];
+  __shared__ float sg_s[D][NB + 1];
+  __shared__ float mx_s[NB];
+  __shared__ bool there_s[NB];
+  const Geom& g = a.pg.g;
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int rg = lane / LPR, cl = lane % LPR;
+  int64_t N = clamp_len(a.seq_lens, b, g.cap) / BS, j0 = (int64_t)blockIdx.x * NB;
+  if (N > g.ncap) N = g.ncap;
+  if (a.prev_lens != nullptr) {
+    const int64_t first = clamp_len(a.prev_lens, b, g.cap) / BS;
+    j0 += first;
+    if (N > first + a.max_new) N = first + a.max_new;
+  }
+  if (j0 >= N) return;
+  const int32_t* row = a.table + (int64_t)b * a.pg.table_stride;
+  for (int jj = w; jj < NB; jj += 4) {
+    const int64_t j = j0 + jj;
+    if (j >= N) break;
+    const int64_t page = page_of(row, j, a.pg.table_blocks, a.pg.pages);
+    if (lane == 0) there_s[jj] = page >= 0;
+    if (page < 0) continue;
+    const uint8_t* p = a.k + page * a.pg.page_stride + (int64_t)h * BS * D + rg * D + 16 * cl;
+    const float scale = a.k_scale[page * a.pg.scale_stride + h];
+    u32x4_t x[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + i * R * D));
+    __builtin_amdgcn_sched_barrier(0);
+    float s[16], n2max = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      float n2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const f32x2_t f = (e & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], true)
+                                  : __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], false);
+        s[e] += f[0];
+        s[e + 1] += f[1];
+        n2 = fmaf(f[0], f[0], n2);
+        n2 = fmaf(f[1], f[1], n2);
+      }
+#pragma unroll
+      for (int o = 1; o < LPR; o <<= 1) n2 += __shfl_xor(n2, o, 64);
+      n2max = fmaxf(n2max, n2);
+      if (n2 != n2) n2max = n2;      // (a row with NaN)
+    }
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = over_rows<LPR>(s[e], [](float p, float q) { return p + q; }) * (1.0f / BS);
+      v[e] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const f32x2_t f = (e & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], true)
+                                  : __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], false);
+        const float d0 = f[0] - s[e], d1 = f[1] - s[e + 1];
+        v[e] = fmaf(d0, d0, v[e]);
+        v[e + 1] = fmaf(d1, d1, v[e + 1]);
+      }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float sd = sqrtf(over_rows<LPR>(v[e], [](float p, float q) { return p + q; }) * (1.0f / BS));
+      if (rg == 0) {
+        mu_s[16 * cl + e][jj] = s[e] * scale;
+        sg_s[16 * cl + e][jj] = sd * scale;
+      }
+    }
+    n2max = over_rows<LPR>(n2max, [](float p, float q) { return p != p ? p : (q != q ? q : fmaxf(p, q)); });
+    if (lane == 0) mx_s[jj] = sqrtf(n2max) * scale;
+  }
+  __syncthreads();
+  const int nv = N - j0 < NB ? (int)(N - j0) : NB;
+  const int64_t bg = (int64_t)b * g.Hkv + h, ob = bg * D * g.ncap + j0;
+  for (int idx = tid; idx < D * NB; idx += 256) {
+    const int i = idx / NB, jj = idx % NB;
+    if (jj >= nv || !there_s[jj]) continue;
+    const int64_t o = ob + (int64_t)i * g.ncap + jj;
+    if (g.stat_dtype == ETA_DT_F16) {
+      reinterpret_cast<_Float16*>(a.mu)[o] = (_Float16)mu_s[i][jj];
+      reinterpret_cast<_Float16*>(a.sigma)[o] = (_Float16)sg_s[i][jj];
+    } else if (g.stat_dtype == ETA_DT_FP8) {
+      reinterpret_cast<uint8_t*>(a.mu)[o] = to_record8(mu_s[i][jj]);
+      reinterpret_cast<uint8_t*>(a.sigma)[o] = to_record8(sg_s[i][jj]);
+    } else {
+      reinterpret_cast<float*>(a.mu)[o] = mu_s[i][jj];
+      reinterpret_cast<float*>(a.sigma)[o] = sg_s[i][jj];
+    }
+  }
+  if (tid < nv && there_s[tid]) a.mx[bg * g.ncap + j0 + tid] = mx_s[tid];
+}
+
+// ---------------------------------------------------------------- copies
+
+// One workgroup for a pair, a head, and K or V: b d codes and their scale.
+__global__ __launch_bounds__(256) void page_copy_kernel(eta_page_pool_t pool, PageGeom pg, const int32_t* src,
+                                                        const int32_t* dst, int64_t n) {
+  const int h = blockIdx.y >> 1;
+  const bool isv = blockIdx.y & 1;
+  const int64_t bytes = (int64_t)pg.g.BS * pg.g.D;
+  uint8_t* code = reinterpret_cast<uint8_t*>(isv ? pool.v : pool.k);
+  float* scale = isv ? pool.v_scale : pool.k_scale;
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int64_t a = src[i], b = dst[i];
+    if (a < 0 || a >= pg.pages || b < 0 || b >= pg.pages) continue;
+    const uint4* from = reinterpret_cast<const uint4*>(code + a * pg.page_stride + h * bytes);
+    uint4* to = reinterpret_cast<uint4*>(code + b * pg.page_stride + h * bytes);
+    for (int k = threadIdx.x; k < bytes / 16; k += 256) to[k] = from[k];
+    if (threadIdx.x == 0) scale[b * pg.scale_stride + h] = scale[a * pg.scale_stride + h];
+  }
+}
+
+// ---------------------------------------------------------------- tables
+//
+// Integer bookkeeping of a few hundred kilobytes at most: what counts is the number of launches
+// and of round trips.  Work over the table's entries is spread over the card; what has to know
+// the order of the free pages runs in one workgroup, which reads refs 4096 pages at a time.
+
+constexpr int kTableThreads = 1024;
+
+// Exclusive prefix over the workgroup's kTableThreads threads; *total gets the sum.
+__device__ __forceinline__ int wide_excl_scan(int x, int* wsum, int* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int incl = wave_incl_scan(x);
+  if (lane == 63) wsum[w] = incl;
+  __syncthreads();
+  int off = 0, tot = 0;
+#pragma unroll
+  for (int k = 0; k < kTableThreads / 64; ++k) {
+    off += k < w ? wsum[k] : 0;
+    tot += wsum[k];
+  }
+  __syncthreads();
+  *total = tot;
+  return off + incl - x;
+}
+
+// Calls f(rank, page) for the pages that `in` holds for, ranks ascending with the pages' numbers
+// from `rank` on, until `most` are found.  Returns the rank after the last.  Every thread of the
+// workgroup takes part.
+template <typename In, typename F>
+__device__ __forceinline__ int64_t ranked(int64_t pages, int64_t most, int* wsum, In in, F f) {
+  int64_t rank = 0;
+  for (int64_t base = 0; base < pages && rank < most; base += 4 * kTableThreads) {
+    bool is[4];
+    int cnt = 0, tot;
+    const int64_t p0 = base + 4 * threadIdx.x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      is[e] = p0 + e < pages && in(p0 + e);
+      cnt += is[e];
+    }
+    int64_t r = rank + wide_excl_scan(cnt, wsum, &tot);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (is[e]) {
+        if (r < most) f(r, p0 + e);
+        ++r;
+      }
+    rank += tot;
+  }
+  return rank;
+}
+
+__device__ __forceinline__ int64_t blocks_of(const eta_table_desc_t& td, int64_t len, int64_t* full) {
+  const int64_t cap = td.table_blocks * td.block_size;
+  len = len < 0 ? 0 : (len > cap ? cap : len);
+  *full = len / td.block_size;
+  return (len + td.block_size - 1) / td.block_size;
+}
+
+// The pages that each row lacks.
+__global__ __launch_bounds__(256) void extend_count_kernel(eta_table_desc_t td, const int32_t* table,
+                                                           const int32_t* seq_lens, int32_t* need) {
+  __shared__ int red[4];
+  const int b = blockIdx.x, tid = threadIdx.x;
+  int64_t full;
+  const int64_t nb = blocks_of(td, seq_lens[b], &full);
+  int cnt = 0;
+  for (int64_t j = tid; j < nb; j += 256) cnt += table[b * td.table_stride + j] < 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) cnt += __shfl_xor(cnt, o, 64);
+  if ((tid & 63) == 0) red[tid >> 6] = cnt;
+  __syncthreads();
+  if (tid == 0) need[b] = red[0] + red[1] + red[2] + red[3];
+}
+
+// Free pages in order (free_list), then row by row the entries that lack one.
+__global__ __launch_bounds__(kTableThreads) void extend_kernel(eta_table_desc_t td, int32_t* table, int32_t* refs,
+                                                               const int32_t* seq_lens, int32_t* missing,
+                                                               int32_t* need, int32_t* free_list) {
+  __shared__ int wsum[kTableThreads / 64];
+  const int tid = threadIdx.x;
+  int64_t want = 0;
+  for (int base = 0; base < td.batch; base += kTableThreads) {
+    int tot;
+    const int x = base + tid < td.batch ? need[base + tid] : 0;
+    const int ex = wide_excl_scan(x, wsum, &tot);
+    // (a row that lacks none is marked, the others get the rank of their first new page)
+    if (base + tid < td.batch) need[base + tid] = x == 0 ? -1 : (int)(want + ex);
+    want += tot;
+  }
+  const int64_t found = ranked(td.num_pages, want, wsum, [&](int64_t p) { return refs[p] <= 0; },
+                               [&](int64_t r, int64_t p) { free_list[r] = (int32_t)p; });
+  const int64_t have = found < want ? found : want;
+  if (tid == 0) missing[0] = (int32_t)(want - have);
+  __threadfence_block();
+  __syncthreads();
+  // a wavefront takes a row, 64 entries at a time
+  for (int b = tid >> 6; b < td.batch; b += kTableThreads / 64) {
+    int64_t r = need[b], full;
+    if (r < 0) continue;
+    const int64_t nb = blocks_of(td, seq_lens[b], &full);
+    for (int64_t j0 = 0; j0 < nb; j0 += 64) {
+      const int64_t j = j0 + (tid & 63);
+      const bool lacks = j < nb && table[b * td.table_stride + j] < 0;
+      const unsigned long long bal = __ballot(lacks);
+      const int64_t k = r + __popcll(bal & ((1ull << (tid & 63)) - 1ull));
+      if (lacks && k < have) {
+        const int32_t p = free_list[k];
+        table[b * td.table_stride + j] = p;
+        refs[p] = 1;
+      }
+      r += __popcll(bal);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void fork_init_kernel(eta_table_desc_t td, const int32_t* refs, int32_t* refs_out) {
+  const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (p < td.num_pages) refs_out[p] = refs[p];
+}
+
+// Rows of the new table and the counts' changes; need[b]: the page to copy for the row, or -1.
+__global__ __launch_bounds__(256) void fork_rows_kernel(eta_table_desc_t td, const int32_t* table,
+                                                        const int32_t* seq_lens, const int32_t* parents,
+                                                        int32_t* table_out, int32_t* refs_out,
+                                                        int32_t* seq_lens_out, int32_t* need) {
+  const int b = blockIdx.y, tid = threadIdx.x;
+  const int64_t j = (int64_t)blockIdx.x * 256 + tid;
+  const int a = parents[b];
+  const bool is = a >= 0 && a < td.batch;
+  const int64_t len = is ? seq_lens[a] : 0;
+  int64_t full;
+  const int64_t nb = blocks_of(td, len, &full);
+  __shared__ int earlier_s;
+  if (tid == 0) earlier_s = 0;
+  __syncthreads();
+  if (is && full < nb) {             // whether an earlier row takes the last block already
+    for (int o = tid; o < b; o += 256)
+      if (parents[o] == a) earlier_s = 1;
+  }
+  __syncthreads();
+  const bool copies = full < nb && earlier_s != 0;
+  if (blockIdx.x == 0 && tid == 0) {
+    const int64_t cap = td.table_blocks * td.block_size;
+    seq_lens_out[b] = (int32_t)(len < 0 ? 0 : (len > cap ? cap : len));
+    const int32_t p = copies ? table[a * td.table_stride + full] : -1;
+    need[b] = p >= 0 && p < td.num_pages ? p : -1;
+  }
+  if (j >= td.table_blocks) return;
+  const int32_t old = table[b * td.table_stride + j];
+  int32_t now = is && j < nb && !(copies && j == full) ? table[a * td.table_stride + j] : -1;
+  if (now < 0 || now >= td.num_pages) now = -1;
+  table_out[b * td.table_stride + j] = now;
+  if (old != now) {
+    if (old >= 0 && old < td.num_pages) atomicSub(refs_out + old, 1);
+    if (now >= 0) atomicAdd(refs_out + now, 1);
+  }
+}
+
+__global__ __launch_bounds__(kTableThreads) void fork_pages_kernel(eta_table_desc_t td, const int32_t* seq_lens_out,
+                                                                   int32_t* table_out, int32_t* refs_out, int32_t* src,
+                                                                   int32_t* dst, int32_t* missing,
+                                                                   const int32_t* need, int32_t* free_list) {
+  __shared__ int wsum[kTableThreads / 64];
+  const int tid = threadIdx.x;
+  int64_t want = 0;
+  for (int base = 0; base < td.batch; base += kTableThreads) {
+    int tot;
+    wide_excl_scan(base + tid < td.batch && need[base + tid] >= 0, wsum, &tot);
+    want += tot;
+  }
+  const int64_t found = ranked(td.num_pages, want, wsum, [&](int64_t p) { return refs_out[p] <= 0; },
+                               [&](int64_t r, int64_t p) { free_list[r] = (int32_t)p; });
+  const int64_t have = found < want ? found : want;
+  if (tid == 0) missing[0] = (int32_t)(want - have);
+  __threadfence_block();
+  __syncthreads();
+  int64_t rank = 0;
+  for (int base = 0; base < td.batch; base += kTableThreads) {
+    const int b = base + tid;
+    const int32_t from = b < td.batch ? need[b] : -1;
+    int tot;
+    const int64_t r = rank + wide_excl_scan(from >= 0, wsum, &tot);
+    if (b < td.batch) {
+      const bool got = from >= 0 && r < have;
+      const int32_t p = got ? free_list[r] : -1;
+      src[b] = got ? from : -1;
+      dst[b] = p;
+      if (got) {
+        int64_t full;
+        blocks_of(td, seq_lens_out[b], &full);
+        table_out[b * td.table_stride + full] = p;
+        refs_out[p] = 1;
+      }
+    }
+    rank += tot;
+  }
+}
+
+// New numbers of the pages (map: -1 for free ones), the counts by them, and the pairs to copy.
+__global__ __launch_bounds__(kTableThreads) void compact_kernel(eta_table_desc_t td, const int32_t* refs,
+                                                                int32_t* refs_out, int32_t* src, int32_t* dst,
+                                                                int32_t* live, int32_t* map) {
+  __shared__ int wsum[kTableThreads / 64];
+  const int tid = threadIdx.x;
+  const int64_t P = td.num_pages;
+  int cnt = 0, n;
+  for (int64_t p = tid; p < P; p += kTableThreads) cnt += refs[p] > 0;
+  wide_excl_scan(cnt, wsum, &n);
+  if (tid == 0) live[0] = n;
+  // free numbers below n, in order, and as many pages in use from n on
+  const int64_t moves = ranked(n, P, wsum, [&](int64_t p) { return refs[p] <= 0; },
+                               [&](int64_t r, int64_t p) { dst[r] = (int32_t)p; });
+  __threadfence_block();
+  __syncthreads();
+  ranked(P - n, P, wsum, [&](int64_t p) { return refs[n + p] > 0; },
+         [&](int64_t r, int64_t p) {
+           const int32_t to = dst[r];
+           src[r] = (int32_t)(n + p);
+           map[n + p] = to;
+           refs_out[to] = refs[n + p];
+         });
+  for (int64_t p = tid; p < P; p += kTableThreads) {
+    const int32_t c = refs[p];
+    if (p < n && c > 0) {
+      map[p] = (int32_t)p;
+      refs_out[p] = c;
+    }
+    if (c <= 0) map[p] = -1;
+    if (p >= n) refs_out[p] = 0;
+  }
+  for (int64_t r = moves + tid; r < P / 2; r += kTableThreads) src[r] = dst[r] = -1;
+}
+
+__global__ __launch_bounds__(256) void compact_table_kernel(eta_table_desc_t td, const int32_t* table,
+                                                            int32_t* table_out, const int32_t* map) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
+  if (j >= td.table_blocks) return;
+  const int32_t p = table[b * td.table_stride + j];
+  table_out[b * td.table_stride + j] = p >= 0 && p < td.num_pages ? map[p] : -1;
+}
+
+template <int D, int BS>
+void launch_store(const StoreArgs& a, bool f32, dim3 grid, hipStream_t stream) {
+  const dim3 threads(D / 8 * (BS / 4));
+  if (f32)
+    hipLaunchKernelGGL((page_store_kernel<D, BS, float>), grid, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL((page_store_kernel<D, BS, uint16_t>), grid, threads, 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_page_store(const PageGeom& pg, const eta_page_pool_t& pool, const int32_t* table,
+                             const eta_page_rows_t& rows, const int32_t* start, const int32_t* new_lens,
+                             hipStream_t stream, LaunchHook hook) {
+  const Geom& g = pg.g;
+  const StoreArgs a{{(uint8_t*)pool.k, (uint8_t*)pool.v}, {pool.k_scale, pool.v_scale}, {rows.k, rows.v},
+                    {rows.k_stride_b, rows.v_stride_b}, {rows.k_stride_h, rows.v_stride_h},
+                    {rows.k_stride_t, rows.v_stride_t}, table, start, new_lens, pg, rows.new_tokens};
+  // the pages that new_tokens tokens can touch, wherever they begin
+  const int64_t touched = ((int64_t)rows.new_tokens + g.BS - 2) / g.BS + 1;
+  const dim3 grid((unsigned)(2 * (touched < pg.table_blocks ? touched : pg.table_blocks)), g.Hkv, g.B);
+  const bool f32 = rows.dtype == ETA_DT_F32;
+  return with_hook(hook, ETA_KERNEL_PAGE_STORE, stream, [&] {
+    if (g.D == 64 && g.BS == 64) launch_store<64, 64>(a, f32, grid, stream);
+    if (g.D == 64 && g.BS == 128) launch_store<64, 128>(a, f32, grid, stream);
+    if (g.D == 128 && g.BS == 64) launch_store<128, 64>(a, f32, grid, stream);
+    if (g.D == 128 && g.BS == 128) launch_store<128, 128>(a, f32, grid, stream);
+  });
+}
+
+hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool, const int32_t* table,
+                                 const int32_t* prev_lens, const int32_t* seq_lens, int max_new,
+                                 const eta_summary_t& s, hipStream_t stream, LaunchHook hook) {
+  const Geom& g = pg.g;
+  const int64_t most = g.cap / g.BS < g.ncap ? g.cap / g.BS : g.ncap;
+  const int64_t nblk = prev_lens != nullptr && max_new < most ? max_new : most;
+  if (nblk <= 0) return hipSuccess;
+  const IndexArgs a{(const uint8_t*)pool.k, pool.k_scale, table, prev_lens, seq_lens, s.mu, s.sigma, s.max_norm, pg, max_new};
+  constexpr int NB = 4;
+  const dim3 grid((unsigned)((nblk + NB - 1) / NB), g.Hkv, g.B);
+  return with_hook(hook, ETA_KERNEL_PAGE_SUMMARIES, stream, [&] {
+#define ETA_PSUM(D_, BS_)       \
+  if (g.D == D_ && g.BS == BS_) \
+    hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, NB>), grid, dim3(256), 0, stream, a);
+    ETA_PSUM(64, 64) ETA_PSUM(64, 128) ETA_PSUM(128, 64) ETA_PSUM(128, 128)
+#undef ETA_PSUM
+  });
+}
+
+hipError_t launch_page_copy(const PageGeom& pg, const eta_page_pool_t& pool, const int32_t* src,
+                            const int32_t* dst, int64_t n, hipStream_t stream, LaunchHook hook) {
+  if (n <= 0) return hipSuccess;
+  const dim3 grid((unsigned)(n < 65536 ? n : 65536), 2 * pg.g.Hkv);
+  return with_hook(hook, ETA_KERNEL_PAGE_COPY, stream, [&] {
+    hipLaunchKernelGGL(page_copy_kernel, grid, dim3(256), 0, stream, pool, pg, src, dst, n);
+  });
+}
+
+hipError_t launch_page_extend(const eta_table_desc_t& td, int32_t* table, int32_t* refs,
+                              const int32_t* seq_lens, int32_t* missing, const TableWs& ws,
+                              hipStream_t stream, LaunchHook hook) {
+  hipError_t e = with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(extend_count_kernel, dim3(td.batch), dim3(256), 0, stream, td, table, seq_lens, ws.need);
+  });
+  if (e != hipSuccess) return e;
+  return with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(extend_kernel, dim3(1), dim3(kTableThreads), 0, stream, td, table, refs, seq_lens, missing,
+                       ws.need, ws.map);
+  });
+}
+
+hipError_t launch_page_fork(const eta_table_desc_t& td, const int32_t* table, const int32_t* refs,
+                            const int32_t* seq_lens, const int32_t* parents, int32_t* table_out,
+                            int32_t* refs_out, int32_t* seq_lens_out, int32_t* src, int32_t* dst,
+                            int32_t* missing, const TableWs& ws, hipStream_t stream, LaunchHook hook) {
+  hipError_t e = with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(fork_init_kernel, dim3((unsigned)((td.num_pages + 255) / 256)), dim3(256), 0, stream, td, refs,
+                       refs_out);
+  });
+  if (e != hipSuccess) return e;
+  e = with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)((td.table_blocks + 255) / 256), td.batch), dim3(256), 0,
+                       stream, td, table, seq_lens, parents, table_out, refs_out, seq_lens_out, ws.need);
+  });
+  if (e != hipSuccess) return e;
+  return with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(fork_pages_kernel, dim3(1), dim3(kTableThreads), 0, stream, td, seq_lens_out, table_out,
+                       refs_out, src, dst, missing, ws.need, ws.map);
+  });
+}
+
+hipError_t launch_page_compact(const eta_table_desc_t& td, const int32_t* table, const int32_t* refs,
+                               int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst,
+                               int32_t* live, const TableWs& ws, hipStream_t stream, LaunchHook hook) {
+  hipError_t e = with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(kTableThreads), 0, stream, td, refs, refs_out, src, dst, live,
+                       ws.map);
+  });
+  if (e != hipSuccess) return e;
+  return with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+    hipLaunchKernelGGL(compact_table_kernel, dim3((unsigned)((td.table_blocks + 255) / 256), td.batch), dim3(256), 0,
+                       stream, td, table, table_out, ws.map);
+  });
+}
+
+}  // namespace eta

@@ -23,7 +23,8 @@ ETA_DT_F32, ETA_DT_BF16, ETA_DT_F16, ETA_DT_FP8 = 0, 1, 2, 3
 KERNEL_KINDS = ("summaries", "predict", "screen", "split_decode", "combine", "dense_split",
                 "dense_combine", "bounds", "calib_accumulate", "calib_solve", "prefill",
                 "qk_rope", "qk_rope_grad", "qk_weight_grad", "prefill_grad_rows", "prefill_grad",
-                "prefill_grad_join")
+                "prefill_grad_join", "page_store", "page_summaries", "page_split",
+                "page_dense_split", "page_table", "page_copy")
 
 _vp = ctypes.c_void_p
 
@@ -72,6 +73,28 @@ class RopeDesc(ctypes.Structure):
                                               "dk_stride_t", "dv_stride_b", "dv_stride_t")]
 
 
+class PageDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "num_q_heads", "num_kv_heads", "head_dim",
+                                              "block_size", "reserved")] + \
+               [(n, ctypes.c_int64) for n in ("num_pages", "table_blocks", "table_stride",
+                                              "page_stride", "scale_stride")]
+
+
+class PagePoolDesc(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
+
+
+class PageRows(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("new_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("k_stride_b", "k_stride_h", "k_stride_t",
+                                              "v_stride_b", "v_stride_h", "v_stride_t")]
+
+
+class TableDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("block_size", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("num_pages", "table_blocks", "table_stride")]
+
+
 class DecodeParams(ctypes.Structure):
     _fields_ = [("beta", ctypes.c_float), ("z", ctypes.c_float), ("offset_a", ctypes.c_float),
                 ("rescue_window_blocks", ctypes.c_int32), ("pin_recent_blocks", ctypes.c_int32),
@@ -91,6 +114,10 @@ EXPORTS = ("eta_build_block_summaries", "eta_build_block_summaries_envelope",
            "eta_gated_prefill_backward_workspace_size", "eta_gated_prefill_backward",
            "eta_qk_norm_rope", "eta_qk_norm_rope_backward_workspace_size",
            "eta_qk_norm_rope_backward", "eta_profile_end_all",
+           "eta_page_store", "eta_page_summaries", "eta_page_decode_workspace_size",
+           "eta_page_decode", "eta_page_decode_predicted", "eta_page_dense_workspace_size",
+           "eta_page_dense_decode", "eta_page_table_workspace_size", "eta_page_extend",
+           "eta_page_fork", "eta_page_compact", "eta_page_copy",
            "eta_last_error_string", "eta_abi_version", "eta_profile_begin", "eta_profile_end")
 
 
@@ -139,6 +166,20 @@ def load_library(path: Optional[str] = None):
         "eta_qk_norm_rope": [P(RopeDesc)] + [_vp] * 12,
         "eta_qk_norm_rope_backward_workspace_size": [P(RopeDesc), P(sz)],
         "eta_qk_norm_rope_backward": [P(RopeDesc)] + [_vp] * 16 + [sz, _vp],
+        "eta_page_store": [P(PageDesc), P(PagePoolDesc), _vp, P(PageRows), _vp, _vp, _vp],
+        "eta_page_summaries": [P(PageDesc), P(PagePoolDesc), _vp, _vp, _vp, i32, P(SummaryDesc), _vp],
+        "eta_page_decode_workspace_size": [P(PageDesc), i64, P(DecodeParams), P(sz)],
+        "eta_page_decode": [P(PageDesc), i32, _vp, P(PagePoolDesc), _vp, _vp, P(SummaryDesc), _vp,
+                            P(DecodeParams), _vp, _vp, _vp, _vp, _vp, sz, _vp],
+        "eta_page_decode_predicted": [P(PageDesc), i32, _vp, P(PagePoolDesc), _vp, _vp, P(SummaryDesc),
+                                      _vp, _vp, P(DecodeParams), _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp],
+        "eta_page_dense_workspace_size": [P(PageDesc), i32, P(sz)],
+        "eta_page_dense_decode": [P(PageDesc), i32, _vp, P(PagePoolDesc), _vp, _vp, _vp, i32, _vp, sz, _vp],
+        "eta_page_table_workspace_size": [P(TableDesc), P(sz)],
+        "eta_page_extend": [P(TableDesc), _vp, _vp, _vp, _vp, _vp, sz, _vp],
+        "eta_page_fork": [P(TableDesc)] + [_vp] * 11 + [sz, _vp],
+        "eta_page_compact": [P(TableDesc)] + [_vp] * 8 + [sz, _vp],
+        "eta_page_copy": [P(PageDesc), P(PagePoolDesc), _vp, _vp, i64, _vp],
         "eta_profile_end_all": [P(KernelTime), i32],
         "eta_profile_begin": [],
         "eta_profile_end": [P(KernelTime)],
@@ -893,3 +934,388 @@ def gated_prefill_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ta
             dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dtau.data_ptr(), workspace.data_ptr(),
             workspace.numel() * workspace.element_size())
     return dq, dk, dv, dtau
+
+
+# ---------------------------------------------------------------- paged 8-bit cache
+#
+# Short calls too: checks, descriptors and workspace sizes are made once for each combination of
+# shapes, strides, types and devices, as above.
+
+E4M3 = torch.float8_e4m3fn
+
+
+@dataclass
+class PagePool:
+    """Pages of one layer's cache: E4M3 codes k [P][Hkv][page][d], v [P][Hkv][d][page] (values lie
+    by dimension) and the scales of each page and head, k_scale, v_scale fp32 [P][Hkv].  A page
+    holds page tokens (64 or 128) of every kv head; pages may be apart (a layer's part of a larger
+    tensor), what a page holds lies together."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @property
+    def page(self) -> int:
+        return self.k.shape[2]
+
+    @staticmethod
+    def empty(num_pages: int, Hkv: int, d: int, page: int, device) -> "PagePool":
+        """A pool with no tokens (codes and scales zero)."""
+        def codes(*shape):
+            return torch.zeros(num_pages, Hkv, *shape, device=device, dtype=torch.uint8).view(E4M3)
+        scales = [torch.zeros(num_pages, Hkv, device=device) for _ in range(2)]
+        return PagePool(codes(page, d), codes(d, page), *scales)
+
+    def _desc(self) -> PagePoolDesc:
+        return PagePoolDesc(k=self.k.data_ptr(), v=self.v.data_ptr(), k_scale=self.k_scale.data_ptr(),
+                            v_scale=self.v_scale.data_ptr())
+
+    def _form(self):
+        return _form(self.k), _form(self.v), _form(self.k_scale), _form(self.v_scale)
+
+
+def _page_desc(pool: PagePool, table: Optional[torch.Tensor], num_q_heads: Optional[int]) -> PageDesc:
+    """The descriptor of a pool (and of a table of its pages), and the checks the C call cannot make."""
+    k, v = pool.k, pool.v
+    if k.dim() != 4 or k.dtype != E4M3:
+        raise ValueError(f"the pool's k must be {E4M3} [P][Hkv][page][d], got {k.dtype} {tuple(k.shape)}")
+    P, Hkv, page, d = k.shape
+    if v.dtype != E4M3 or tuple(v.shape) != (P, Hkv, d, page):
+        raise ValueError(f"the pool's v must be {E4M3} {(P, Hkv, d, page)}, got {v.dtype} {tuple(v.shape)}")
+    for name, t in (("k", k), ("v", v)):
+        if not t[:1].is_contiguous():
+            raise ValueError(f"the pool's {name}: what a page holds must be contiguous")
+    if P > 1 and k.stride(0) != v.stride(0):
+        raise ValueError("the pool's k and v must have the same strides between pages")
+    for name, t in (("k_scale", pool.k_scale), ("v_scale", pool.v_scale)):
+        if t.dtype != torch.float32 or tuple(t.shape) != (P, Hkv) or not t[:1].is_contiguous():
+            raise ValueError(f"{name} must be fp32 {(P, Hkv)}, a page's scales contiguous, got {t.dtype} {tuple(t.shape)}")
+    if P > 1 and pool.k_scale.stride(0) != pool.v_scale.stride(0):
+        raise ValueError("k_scale and v_scale must have the same strides between pages")
+    pd = PageDesc(batch=1, num_q_heads=Hkv if num_q_heads is None else num_q_heads, num_kv_heads=Hkv, head_dim=d,
+                  block_size=page, num_pages=P, table_blocks=1, table_stride=1,
+                  page_stride=k.stride(0) if P > 1 else Hkv * page * d,
+                  scale_stride=pool.k_scale.stride(0) if P > 1 else Hkv)
+    if table is not None:
+        _table("table", table)
+        pd.batch, pd.table_blocks = table.shape
+        pd.table_stride = table.stride(0) if table.shape[0] > 1 else table.shape[1]
+    return pd
+
+
+def _table(name: str, t: torch.Tensor, shape=None) -> None:
+    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) \
+            or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be int32 [B][blocks]{'' if shape is None else f' {tuple(shape)}'}, a row's "
+                         f"entries contiguous, got {t.dtype} {tuple(t.shape)}")
+
+
+def _index_shape(summ: Summaries, B: int, Hkv: int, d: int) -> None:
+    n = summ.n_blk_cap
+    for name, t, shape in (("mu", summ.mu, (B, Hkv, d, n)), ("sigma", summ.sigma, (B, Hkv, d, n)),
+                           ("max_norm", summ.max_norm, (B, Hkv, n))):
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"the index's {name} must be {shape} contiguous, got {tuple(t.shape)}")
+    if summ.mu.dtype != summ.sigma.dtype or summ.mu.dtype not in (torch.float32, torch.float16, E4M3) \
+            or summ.max_norm.dtype != torch.float32:
+        raise TypeError(f"unsupported record dtypes {summ.mu.dtype}, {summ.sigma.dtype}, {summ.max_norm.dtype}")
+
+
+def _query(q: torch.Tensor, pool: PagePool, table: torch.Tensor):
+    """Checks of a decode call's q [B][Hq][d]; the device."""
+    _dtype_code(q)
+    if q.dim() != 3 or not q.is_contiguous() or q.shape[0] != table.shape[0] or q.shape[2] != pool.k.shape[3]:
+        raise ValueError(f"q must be [{table.shape[0]}][Hq][{pool.k.shape[3]}] contiguous, got {tuple(q.shape)}")
+
+
+def _summ_form(s: Summaries):
+    return _form(s.mu), _form(s.sigma), _form(s.max_norm)
+
+
+def store_pages(k: torch.Tensor, v: torch.Tensor, pool: PagePool, table: torch.Tensor, *,
+                start: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
+                stream=None) -> PagePool:
+    """eta_page_store: rounds new keys and values k, v [B][Hkv][T][d] (float32 or bfloat16, any
+    strides, the head dimension contiguous) into the pages that table int32 [B][blocks] lists:
+    token i of sequence b at position start[b] + i, for i < new_lens[b] (None: 0 and T).  Returns
+    the pool, changed in place."""
+    def make():
+        dt = _dtype_code(k)
+        dev = _on_one_gpu(k, v, pool.k, pool.v, pool.k_scale, pool.v_scale, table, start, new_lens)
+        pd = _page_desc(pool, table, None)
+        B, Hkv, d = pd.batch, pd.num_kv_heads, pd.head_dim
+        for name, t in (("k", k), ("v", v)):
+            if t.dim() != 4 or t.dtype != k.dtype or (t.shape[0], t.shape[1], t.shape[3]) != (B, Hkv, d) \
+                    or t.shape[2] != k.shape[2] or t.stride(3) != 1:
+                raise ValueError(f"{name} must be {k.dtype} [{B}][{Hkv}][T][{d}], the head dimension contiguous, got "
+                                 f"{t.dtype} {tuple(t.shape)}")
+        _vector("start", start, B, torch.int32)
+        _vector("new_lens", new_lens, B, torch.int32)
+        steps = {f"{n}_stride_{x}": _step(t, i) for n, t in (("k", k), ("v", v)) for i, x in enumerate("bht")}
+        return pd, ctypes.byref(pd), dev, dict(new_tokens=k.shape[2], dtype=dt, **steps)
+    _, ref, dev, rows = _plan((3, _form(k), _form(v), pool._form(), _form(table), _form(start), _form(new_lens)), make)
+    r = PageRows(k=k.data_ptr(), v=v.data_ptr(), **rows)
+    _launch(load_library().eta_page_store, dev, stream, ref, ctypes.byref(pool._desc()), table.data_ptr(),
+            ctypes.byref(r), _at(start), _at(new_lens))
+    return pool
+
+
+def build_page_summaries(pool: PagePool, table: torch.Tensor, seq_lens: torch.Tensor, *,
+                         out: Optional[Summaries] = None, stat_dtype: torch.dtype = torch.float32,
+                         stream=None) -> Summaries:
+    """eta_page_summaries: the block index (mu, sigma, M) of the keys as the pages hold them."""
+    if out is None:
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = Summaries.empty(table.shape[0], pool.k.shape[1], pool.k.shape[3], table.shape[1], pool.k.device,
+                                  stat_dtype)
+        _shared(stream, out.mu, out.sigma, out.max_norm)
+    return _page_summaries(pool, table, None, seq_lens, 0, out, stream)
+
+
+def update_page_summaries(pool: PagePool, table: torch.Tensor, prev_lens: torch.Tensor, seq_lens: torch.Tensor,
+                          summ: Summaries, *, max_new_blocks: int = 1, stream=None) -> Summaries:
+    """eta_page_summaries with prev_lens: records of the (at most max_new_blocks) blocks of each
+    sequence that were completed since."""
+    if prev_lens is None:
+        raise ValueError("prev_lens must be given")
+    return _page_summaries(pool, table, prev_lens, seq_lens, max_new_blocks, summ, stream)
+
+
+def _page_summaries(pool, table, prev_lens, seq_lens, max_new, summ, stream):
+    def make():
+        dev = _on_one_gpu(pool.k, pool.v, pool.k_scale, pool.v_scale, table, prev_lens, seq_lens, summ.mu, summ.sigma,
+                          summ.max_norm)
+        pd = _page_desc(pool, table, None)
+        _vector("seq_lens", seq_lens, pd.batch, torch.int32)
+        _vector("prev_lens", prev_lens, pd.batch, torch.int32)
+        _index_shape(summ, pd.batch, pd.num_kv_heads, pd.head_dim)
+        return pd, ctypes.byref(pd), dev
+    _, ref, dev = _plan((4, pool._form(), _form(table), _form(prev_lens), _form(seq_lens), _summ_form(summ)), make)
+    _launch(load_library().eta_page_summaries, dev, stream, ref, ctypes.byref(pool._desc()), table.data_ptr(),
+            _at(prev_lens), seq_lens.data_ptr(), int(max_new), ctypes.byref(summ.desc()))
+    return summ
+
+
+def _decode_pages(q, pool, table, seq_lens, summ, tau, W, bias, params, out, mask, counts, union_counts, tau_out,
+                  want_counts, workspace, stream):
+    p = params if params is not None else decode_params()
+
+    def make():
+        dev = _on_one_gpu(q, pool.k, pool.v, pool.k_scale, pool.v_scale, table, seq_lens, summ.mu, summ.sigma,
+                          summ.max_norm, tau, W, bias, out, mask, counts, union_counts, tau_out, workspace)
+        _table("table", table)
+        _query(q, pool, table)
+        B, Hq, d = q.shape
+        pd = _page_desc(pool, table, Hq)
+        _vector("seq_lens", seq_lens, B, torch.int32)
+        _index_shape(summ, B, pd.num_kv_heads, d)
+        _plain("tau", tau, (B, Hq), torch.float32)
+        if bias is not None:
+            _check_predictor(q, W, bias)
+        _plain("tau_out", tau_out, (B, Hq), torch.float32)
+        _plain("out", out, q.shape, q.dtype)
+        _plain("mask", mask, (B, Hq, summ.n_blk_cap), torch.uint8)
+        _plain("counts", counts, (B, Hq), torch.int32)
+        _plain("union_counts", union_counts, (B, pd.num_kv_heads), torch.int32)
+        n = ctypes.c_size_t()
+        _check(load_library().eta_page_decode_workspace_size(ctypes.byref(pd), summ.n_blk_cap, ctypes.byref(p),
+                                                             ctypes.byref(n)))
+        return pd, ctypes.byref(pd), dev, n.value, _dtype_code(q)
+    # (the workspace's size goes by num_splits alone of the parameters; the rest is checked in the call)
+    _, ref, dev, nbytes, dt = _plan(
+        (5, p.num_splits, _form(q), pool._form(), _form(table), _form(seq_lens), _summ_form(summ), _form(tau), _form(W),
+         _form(bias), _form(out), _form(mask), _form(counts), _form(union_counts), _form(tau_out), _form(workspace)), make)
+    out, mask, counts, union_counts = _decode_outputs(q, pool.k, summ, out, mask, counts, union_counts, want_counts,
+                                                      stream)
+    workspace = _workspace(workspace, nbytes, dev, stream)
+    lib, common = load_library(), (dt, q.data_ptr(), ctypes.byref(pool._desc()), table.data_ptr(), seq_lens.data_ptr(),
+                                   ctypes.byref(summ.desc()))
+    results = (ctypes.byref(p), out.data_ptr(), mask.data_ptr(), _at(counts), _at(union_counts))
+    space = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    if bias is None:
+        _launch(lib.eta_page_decode, dev, stream, ref, *common, tau.data_ptr(), *results, *space)
+    else:
+        _launch(lib.eta_page_decode_predicted, dev, stream, ref, *common, _at(W), bias.data_ptr(), *results,
+                _at(tau_out), *space)
+    return DecodeOut(out=out, mask=mask, counts=counts, union_counts=union_counts)
+
+
+def decode_pages(q: torch.Tensor, pool: PagePool, table: torch.Tensor, seq_lens: torch.Tensor, summ: Summaries,
+                 tau: torch.Tensor, *, params: Optional[DecodeParams] = None, out=None, mask=None, counts=None,
+                 union_counts=None, want_counts: bool = True, workspace: Optional[torch.Tensor] = None,
+                 stream=None) -> DecodeOut:
+    """eta_page_decode: one ETA decode step over pages (decode's results; q [B][Hq][d], table int32
+    [B][blocks], summ as build_page_summaries gives it, tau fp32 [B][Hq])."""
+    if tau is None:
+        raise ValueError("tau must be given")
+    return _decode_pages(q, pool, table, seq_lens, summ, tau, None, None, params, out, mask, counts, union_counts, None,
+                         want_counts, workspace, stream)
+
+
+def decode_pages_predicted(q: torch.Tensor, pool: PagePool, table: torch.Tensor, seq_lens: torch.Tensor,
+                           summ: Summaries, W: Optional[torch.Tensor], bias: torch.Tensor, *,
+                           params: Optional[DecodeParams] = None, out=None, mask=None, counts=None,
+                           union_counts=None, tau_out=None, want_counts: bool = True,
+                           workspace: Optional[torch.Tensor] = None, stream=None) -> DecodeOut:
+    """eta_page_decode_predicted: the step with the thresholds predicted in it (W, bias as in
+    predict_threshold)."""
+    if bias is None:
+        raise ValueError("bias must be given")
+    return _decode_pages(q, pool, table, seq_lens, summ, None, W, bias, params, out, mask, counts, union_counts,
+                         tau_out, want_counts, workspace, stream)
+
+
+def dense_decode_pages(q: torch.Tensor, pool: PagePool, table: torch.Tensor, seq_lens: torch.Tensor, *,
+                       num_splits: int = 0, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """eta_page_dense_decode: plain softmax attention over every token of the pages."""
+    def make():
+        dev = _on_one_gpu(q, pool.k, pool.v, pool.k_scale, pool.v_scale, table, seq_lens, out, workspace)
+        _table("table", table)
+        _query(q, pool, table)
+        pd = _page_desc(pool, table, q.shape[1])
+        _vector("seq_lens", seq_lens, pd.batch, torch.int32)
+        _plain("out", out, q.shape, q.dtype)
+        n = ctypes.c_size_t()
+        _check(load_library().eta_page_dense_workspace_size(ctypes.byref(pd), num_splits, ctypes.byref(n)))
+        return pd, ctypes.byref(pd), dev, n.value, _dtype_code(q)
+    num_splits = int(num_splits)
+    _, ref, dev, nbytes, dt = _plan((6, num_splits, _form(q), pool._form(), _form(table), _form(seq_lens), _form(out),
+                                     _form(workspace)), make)
+    if out is None:
+        out = _empty_like(stream, q)
+    workspace = _workspace(workspace, nbytes, dev, stream)
+    _launch(load_library().eta_page_dense_decode, dev, stream, ref, dt, q.data_ptr(), ctypes.byref(pool._desc()),
+            table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), num_splits, workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())
+    return out
+
+
+@dataclass
+class PageFork:
+    """fork_pages' results: the new table, counts and lengths, the copies to make (src -> dst, -1:
+    none) and how many rows found no free page."""
+    table: torch.Tensor          # int32 [B][blocks]
+    refs: torch.Tensor           # int32 [P]
+    seq_lens: torch.Tensor       # int32 [B]
+    src: torch.Tensor            # int32 [B]
+    dst: torch.Tensor            # int32 [B]
+    missing: torch.Tensor        # int32 [1]
+
+
+@dataclass
+class PageCompaction:
+    """compact_pages' results: the new table and counts, the copies to make (src -> dst, -1 behind
+    the last) and the number of pages in use."""
+    table: torch.Tensor          # int32 [B][blocks]
+    refs: torch.Tensor           # int32 [P]
+    src: torch.Tensor            # int32 [P / 2]
+    dst: torch.Tensor            # int32 [P / 2]
+    live: torch.Tensor           # int32 [1]
+
+
+def _table_plan(key: int, page: int, tables, refs, vectors, given):
+    """Descriptor, device and workspace size of a page-table call."""
+    def make():
+        dev = _on_one_gpu(*tables, *refs, *(t for _, t, _ in vectors), *given)
+        table = tables[0]
+        B, n = table.shape
+        for t in tables:
+            if t is not None:
+                _table("a table", t, (B, n))
+                if B > 1 and t.stride(0) != table.stride(0):
+                    raise ValueError("the tables must have the same strides")
+        P = refs[0].numel()
+        for t in refs:
+            _vector("refs", t, P, torch.int32)
+        for name, t, m in vectors:
+            _vector(name, t, B if m is None else m, torch.int32)
+        td = TableDesc(batch=B, block_size=page, num_pages=P, table_blocks=n,
+                       table_stride=table.stride(0) if B > 1 else n)
+        size = ctypes.c_size_t()
+        _check(load_library().eta_page_table_workspace_size(ctypes.byref(td), ctypes.byref(size)))
+        return td, ctypes.byref(td), dev, size.value
+    return _plan((key, page, *map(_form, tables), *map(_form, refs), *(_form(t) for _, t, _ in vectors),
+                  *map(_form, given)), make)
+
+
+def extend_pages(table: torch.Tensor, refs: torch.Tensor, seq_lens: torch.Tensor, *, page: int,
+                 missing: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+    """eta_page_extend: a page for every block of table int32 [B][blocks] that has tokens
+    (lengths seq_lens int32 [B], page tokens each) and none yet (a negative entry), counted in
+    refs int32 [P]; both change in place.  Returns how many found no free page, int32 [1]."""
+    _, ref, dev, nbytes = _table_plan(7, int(page), (table,), (refs,),
+                                      (("seq_lens", seq_lens, None), ("missing", missing, 1)), (workspace,))
+    if missing is None:
+        missing = _empty(stream, dev, torch.int32, 1)
+    workspace = _workspace(workspace, nbytes, dev, stream)
+    _launch(load_library().eta_page_extend, dev, stream, ref, table.data_ptr(), refs.data_ptr(), seq_lens.data_ptr(),
+            missing.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return missing
+
+
+def fork_pages(table: torch.Tensor, refs: torch.Tensor, seq_lens: torch.Tensor, parents: torch.Tensor, *, page: int,
+               out: Optional[PageFork] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> PageFork:
+    """eta_page_fork: row b of the new table goes on from row parents[b] of the present one (int32
+    [B]; outside [0, B): empty).  Full pages are shared; a last page that is not full is copied for
+    every row but the first that takes it (copy_pages makes the copies, for each layer's pool); the
+    pages that no row goes on with become free.  table, refs and seq_lens are left as they are."""
+    o = out
+    _, ref, dev, nbytes = _table_plan(
+        8, int(page), (table, o and o.table), (refs, o and o.refs),
+        (("seq_lens", seq_lens, None), ("parents", parents, None), ("seq_lens", o and o.seq_lens, None),
+         ("src", o and o.src, None), ("dst", o and o.dst, None), ("missing", o and o.missing, 1)), (workspace,))
+    if o is None:
+        B = table.shape[0]
+        o = PageFork(_like_table(stream, table), _empty_like(stream, refs),
+                     *(_empty(stream, dev, torch.int32, m) for m in (B, B, B, 1)))
+    workspace = _workspace(workspace, nbytes, dev, stream)
+    _launch(load_library().eta_page_fork, dev, stream, ref, table.data_ptr(), refs.data_ptr(), seq_lens.data_ptr(),
+            parents.data_ptr(), o.table.data_ptr(), o.refs.data_ptr(), o.seq_lens.data_ptr(), o.src.data_ptr(),
+            o.dst.data_ptr(), o.missing.data_ptr(), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())
+    return o
+
+
+def compact_pages(table: torch.Tensor, refs: torch.Tensor, *, out: Optional[PageCompaction] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> PageCompaction:
+    """eta_page_compact: renumbers the pages so that those in use (refs > 0) are the first;
+    copy_pages makes the copies, for each layer's pool.  table and refs are left as they are."""
+    o = out
+    half = refs.numel() // 2
+    _, ref, dev, nbytes = _table_plan(9, 1, (table, o and o.table), (refs, o and o.refs),
+                                      (("src", o and o.src, half), ("dst", o and o.dst, half),
+                                       ("live", o and o.live, 1)), (workspace,))
+    if o is None:
+        o = PageCompaction(_like_table(stream, table), _empty_like(stream, refs),
+                           *(_empty(stream, dev, torch.int32, m) for m in (half, half, 1)))
+    workspace = _workspace(workspace, nbytes, dev, stream)
+    _launch(load_library().eta_page_compact, dev, stream, ref, table.data_ptr(), refs.data_ptr(), o.table.data_ptr(),
+            o.refs.data_ptr(), o.src.data_ptr(), o.dst.data_ptr(), o.live.data_ptr(), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())
+    return o
+
+
+def _like_table(stream, table: torch.Tensor) -> torch.Tensor:
+    """A new table of the same shape and distance between rows."""
+    B, n = table.shape
+    step = table.stride(0) if B > 1 else n
+    t = _empty(stream, table.device, torch.int32, B, step)
+    return t[:, :n] if step != n else t
+
+
+def copy_pages(pool: PagePool, src: torch.Tensor, dst: torch.Tensor, *, stream=None) -> PagePool:
+    """eta_page_copy: page src[i] over page dst[i] (int32 [n] each; pairs with a number that is no
+    page are passed over), codes and scales.  Returns the pool, changed in place."""
+    def make():
+        dev = _on_one_gpu(pool.k, pool.v, pool.k_scale, pool.v_scale, src, dst)
+        _vector("src", src, src.numel(), torch.int32)
+        _vector("dst", dst, src.numel(), torch.int32)
+        pd = _page_desc(pool, None, None)
+        return pd, ctypes.byref(pd), dev
+    _, ref, dev = _plan((10, pool._form(), _form(src), _form(dst)), make)
+    _launch(load_library().eta_page_copy, dev, stream, ref, ctypes.byref(pool._desc()), src.data_ptr(), dst.data_ptr(),
+            src.numel())
+    return pool
