@@ -42,7 +42,7 @@ def hipcc() -> str:
 # (no copies between accumulation and arithmetic registers there; the
 # calibration kernel is faster with the default register classes, and the
 # prefill's gradients, at 256 registers a wavefront, get the same code from them)
-VGPR_FORM = {"eta_prefill.hip"}
+VGPR_FORM = {"eta_prefill.hip", "eta_page.hip", "eta_page_attend.hip"}
 
 
 def _flags(src: str):

@@ -7,12 +7,27 @@
 #include "eta_device.h"
 #include "eta_lanes.h"
 #include "eta_page.h"
+#include "eta_page_codes.h"
 
 namespace eta {
 namespace {
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef int64_t i64x2_t __attribute__((ext_vector_type(2)));
+
+// the largest value over the wavefront, in every lane
+__device__ __forceinline__ float wave_max64(float x) {
+  auto over = [&](uint32_t y) { x = fmaxf(x, __uint_as_float(y)); };
+  over(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0xB1, 0xf, 0xf, false));    // quad_perm [1,0,3,2]
+  over(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x4E, 0xf, 0xf, false));    // quad_perm [2,3,0,1]
+  over(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x141, 0xf, 0xf, false));   // row_half_mirror
+  over(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x140, 0xf, 0xf, false));   // row_mirror
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 // ---------------------------------------------------------------- storing
 //
@@ -122,8 +137,7 @@ __global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs 
 #pragma unroll
     for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_abs(x[r][e]));
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
+  amax = wave_max64(amax);
   if ((tid & 63) == 0) red_s[tid >> 6] = amax;
   __syncthreads();
 #pragma unroll
@@ -182,23 +196,22 @@ __global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs 
 
 // ---------------------------------------------------------------- the index
 //
-// Wavefront w of a workgroup takes blocks w, w + 4, .. of its NB: a load covers whole rows (LPR
-// lanes of 16 codes), the block stays in registers for both passes (mean, then the mean squared
-// deviation from it), the rows' norms are summed over a row's lanes.  Sums run on the codes; the
-// page's scale is applied once.  Results leave as rows of the dimension-major records.
-
-// the sum (or maximum) over lanes l, l ^ N, l ^ 2 N, .. in every lane
-template <int N, typename Op>
-__device__ __forceinline__ float over_rows(float x, Op op) {
-#pragma unroll
-  for (int o = N; o < 64; o <<= 1) x = op(x, __shfl_xor(x, o, 64));
-  return x;
-}
-
-__device__ __forceinline__ uint8_t to_record8(float f) {     // saturating at 448, NaN stays
-  const float a = fabsf(f) > 448.0f ? copysignf(448.0f, f) : f;
-  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, a, 0, false);
-}
+// mu = s m, sigma = s sqrt(mean((c - m)^2)), M = s max |c_t| over the codes c of a block, m their
+// mean and s the page's scale.  A byte read would cost the vector unit five operations (widen
+// twice, add, subtract, square, and the row's norm), about what it can do in the time HBM takes
+// for it; the matrix cores take all but the square.  A tile of 16 tokens x 32 dims of codes, as
+// it is loaded, is the A operand of
+//   A I     against columns of the unit matrix: the codes widened, each 16 dims a result whose
+//           rows are the tile's tokens; added up over the tiles in the accumulator (the sums are
+//           exact: codes are multiples of 2^-9), and in the second pass, with -m as the
+//           accumulator's start, the deviations;
+//   A A^T   the tokens' products, whose diagonal has the squared norms: of rows of 64 dims no
+//           element is larger than the largest of them, so nothing looks for it; the two parts
+//           of rows of 128 are added.  (With the codes widened to bf16: sums of 8-bit products
+//           come back 5e-6 off, of bf16 ones 3e-8.)
+// The block stays in registers for both passes (two passes: mean first, so that a coordinate
+// whose mean is far larger than its spread loses nothing).  Results are staged in LDS and leave
+// as rows of the dimension-major records.
 
 struct IndexArgs {
   const uint8_t* k;
@@ -213,17 +226,27 @@ struct IndexArgs {
   int max_new;
 };
 
-template <int D, int BS, int NB>
-__global__ __launch_bounds__(256) void page_summaries_kernel(IndexArgs a) {
-  constexpr int LPR = D / 16, R = 64 / LPR, NI = BS / R;
+// fp32 -> E4M3, nearest even, saturating at 448; NaN stays
+__device__ __forceinline__ uint8_t to_record8(float f) {
+  const float a = fabsf(f) > 448.0f ? copysignf(448.0f, f) : f;
+  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, a, 0, false);
+}
+
+template <int D, int BS, int NB, bool STREAM>
+__global__ __launch_bounds__(256, 2) void page_summaries_kernel(IndexArgs a) {
+  constexpr int HALF = D / 64, RT = 16 / HALF;         // parts of a row, tokens of a load
+  constexpr int NL = BS / RT;                          // loads of a block
   __shared__ float mu_s[D][NB + 1];
   __shared__ float sg_s[D][NB + 1];
   __shared__ float mx_s[NB];
   __shared__ bool there_s[NB];
   const Geom& g = a.pg.g;
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int rg = lane / LPR, cl = lane % LPR;
-  int64_t N = clamp_len(a.seq_lens, b, g.cap) / BS, j0 = (int64_t)blockIdx.x * NB;
+  const int col = lane & 15, g4 = lane >> 4;
+  // workgroups go to the XCDs round robin: each XCD takes a run of neighbours, whose records
+  // share cache lines
+  const int per = gridDim.x / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  int64_t N = clamp_len(a.seq_lens, b, g.cap) / BS, j0 = (int64_t)at * NB;
   if (N > g.ncap) N = g.ncap;
   if (a.prev_lens != nullptr) {
     const int64_t first = clamp_len(a.prev_lens, b, g.cap) / BS;
@@ -231,65 +254,116 @@ __global__ __launch_bounds__(256) void page_summaries_kernel(IndexArgs a) {
     if (N > first + a.max_new) N = first + a.max_new;
   }
   if (j0 >= N) return;
+  // columns 16 u .. of the unit matrix of a step's 32 dims: this lane's rows are 8 g4 .. + 7
+  int64_t unit[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = 16 * u + col - 8 * g4;
+    unit[u] = i >= 0 && i < 8 ? (int64_t)0x38 << (8 * i) : 0;      // 0x38: 1.0
+  }
+  // 1 where register r of a 16 x 16 result is the lane's element of the diagonal
+  float diag[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) diag[r] = col == 4 * g4 + r ? 1.0f : 0.f;
   const int32_t* row = a.table + (int64_t)b * a.pg.table_stride;
-  for (int jj = w; jj < NB; jj += 4) {
+  // Block jj of this workgroup; its loads (row i of the A operand: token i % RT, part i / RT of
+  // its row, so that a load covers whole rows) are in flight while the wavefront's block before
+  // it is worked on.  Returns whether it is there.
+  float scale_n = 0.f;
+  i64x2_t x[NL], xn[NL];
+  auto load = [&](int jj) {
     const int64_t j = j0 + jj;
-    if (j >= N) break;
+    if (jj >= NB || j >= N) return false;
     const int64_t page = page_of(row, j, a.pg.table_blocks, a.pg.pages);
     if (lane == 0) there_s[jj] = page >= 0;
-    if (page < 0) continue;
-    const uint8_t* p = a.k + page * a.pg.page_stride + (int64_t)h * BS * D + rg * D + 16 * cl;
-    const float scale = a.k_scale[page * a.pg.scale_stride + h];
-    u32x4_t x[NI];
+    const int64_t from = page < 0 ? 0 : page;          // (no page: another is read and not recorded)
+    const uint8_t* p = a.k + from * a.pg.page_stride + (int64_t)h * BS * D + (col % RT) * D + (col / RT) * 64 + 16 * g4;
+    scale_n = a.k_scale[from * a.pg.scale_stride + h];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + i * R * D));
+    for (int t = 0; t < NL; ++t) {
+      const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + t * RT * D);
+      xn[t] = __builtin_bit_cast(i64x2_t, STREAM ? __builtin_nontemporal_load(q) : *q);
+    }
+    return true;
+  };
+  bool more = load(w);
+  for (int jj = w; more; jj += 4) {
+    const float scale = scale_n;
+#pragma unroll
+    for (int t = 0; t < NL; ++t) x[t] = xn[t];
+    more = NB > 4 && load(jj + 4);
     __builtin_amdgcn_sched_barrier(0);
-    float s[16], n2max = 0.f;
+    float n2 = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    for (int t = 0; t < NL; ++t) {
+      f32x4 aa = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      float n2 = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const f32x2_t f = (e & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], true)
-                                  : __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], false);
-        s[e] += f[0];
-        s[e + 1] += f[1];
-        n2 = fmaf(f[0], f[0], n2);
-        n2 = fmaf(f[1], f[1], n2);
+      for (int e = 0; e < 2; ++e) {
+        const bf16x8 wide = widen((uint32_t)x[t][e], (uint32_t)(x[t][e] >> 32));
+        aa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, wide, aa, 0, 0, 0);
       }
+      if constexpr (HALF == 1) {
 #pragma unroll
-      for (int o = 1; o < LPR; o <<= 1) n2 += __shfl_xor(n2, o, 64);
-      n2max = fmaxf(n2max, n2);
-      if (n2 != n2) n2max = n2;      // (a row with NaN)
-    }
-    float v[16];
+        for (int r = 0; r < 4; ++r) n2 = fmaxf(n2, aa[r]);
+      } else {
+        // the diagonal's element of a token's first part is in lane (token, row token / 4), that
+        // of its second in (8 + token, row 2 + token / 4); every other lane has 0
+        float y = aa[0] * diag[0];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[e] = over_rows<LPR>(s[e], [](float p, float q) { return p + q; }) * (1.0f / BS);
-      v[e] = 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const f32x2_t f = (e & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], true)
-                                  : __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][e / 4], false);
-        const float d0 = f[0] - s[e], d1 = f[1] - s[e + 1];
-        v[e] = fmaf(d0, d0, v[e]);
-        v[e + 1] = fmaf(d1, d1, v[e + 1]);
-      }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float sd = sqrtf(over_rows<LPR>(v[e], [](float p, float q) { return p + q; }) * (1.0f / BS));
-      if (rg == 0) {
-        mu_s[16 * cl + e][jj] = s[e] * scale;
-        sg_s[16 * cl + e][jj] = sd * scale;
+        for (int r = 1; r < 4; ++r) y = fmaf(aa[r], diag[r], y);
+        y = dpp_add<0x128>(y);                         // row_ror:8
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+        n2 = fmaxf(n2, __uint_as_float(r[0]) + __uint_as_float(r[1]));
       }
     }
-    n2max = over_rows<LPR>(n2max, [](float p, float q) { return p != p ? p : (q != q ? q : fmaxf(p, q)); });
-    if (lane == 0) mx_s[jj] = sqrtf(n2max) * scale;
+    // the sum over the lanes of a column that hold the same part of a row, in each of them
+    auto column_sum = [](float y) {
+      auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+      y = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+      if constexpr (HALF == 1) {
+        r = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+        y = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+      }
+      return y;
+    };
+    // step e, columns u: dim 16 (2 u + col / 8) + 8 e + col % 8 of the lane's part
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      __builtin_amdgcn_sched_barrier(0);               // (32 dims at a time: few registers)
+      f32x4 y[2], from[2];
+      float v[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < NL; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) y[u] = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(x[t][e], unit[u], y[u], 0, 0, 0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float mean = column_sum((y[u][0] + y[u][1]) + (y[u][2] + y[u][3])) * (1.0f / BS);
+        from[u] = f32x4{-mean, -mean, -mean, -mean};
+        v[u] = 0.f;
+      }
+#pragma unroll
+      for (int t = 0; t < NL; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(x[t][e], unit[u], from[u], 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[u] = fmaf(d[r], d[r], v[u]);
+        }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float sd = sqrtf(column_sum(v[u]) * (1.0f / BS));
+        if (HALF == 1 ? g4 == 0 : (g4 & 1) == 0) {
+          const int i = 64 * (g4 >> 1) + 16 * (2 * u + (col >> 3)) + 8 * e + (col & 7);
+          mu_s[i][jj] = -from[u][0] * scale;
+          sg_s[i][jj] = sd * scale;
+        }
+      }
+    }
+    n2 = wave_max64(n2);
+    if (lane == 0) mx_s[jj] = sqrtf(n2) * scale;
   }
   __syncthreads();
   const int nv = N - j0 < NB ? (int)(N - j0) : NB;
@@ -612,12 +686,22 @@ hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool
   const int64_t nblk = prev_lens != nullptr && max_new < most ? max_new : most;
   if (nblk <= 0) return hipSuccess;
   const IndexArgs a{(const uint8_t*)pool.k, pool.k_scale, table, prev_lens, seq_lens, s.mu, s.sigma, s.max_norm, pg, max_new};
-  constexpr int NB = 4;
-  const dim3 grid((unsigned)((nblk + NB - 1) / NB), g.Hkv, g.B);
+  // Large caches (past what the last-level cache holds): 32 blocks to a workgroup, whose records
+  // leave as whole rows, the keys read past the caches.  Below, one block to a wavefront, four to a
+  // workgroup, so that as many start as there are.  us with 32 and the hint / 4 without, fp32
+  // records: 256 MiB of keys (128 x 128 blocks) 57 / 69; 469 MiB (128 dims x 64) 111 / 117, 469 MiB
+  // (64 x 64) 114 / 119; 98 MiB (128 x 64) 33 / 29; 49 MiB (64 x 128) 20 / 14; 4 MiB 23 / 7.
+  const bool large = nblk >= 32 && nblk * g.Hkv * g.B * g.BS * g.D > (int64_t(200) << 20);
+  const int nb = large ? 32 : 4;
+  const dim3 grid((unsigned)((nblk + 8 * nb - 1) / (8 * nb) * 8), g.Hkv, g.B);
   return with_hook(hook, ETA_KERNEL_PAGE_SUMMARIES, stream, [&] {
-#define ETA_PSUM(D_, BS_)       \
-  if (g.D == D_ && g.BS == BS_) \
-    hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, NB>), grid, dim3(256), 0, stream, a);
+#define ETA_PSUM(D_, BS_)                                                                                    \
+  if (g.D == D_ && g.BS == BS_) {                                                                            \
+    if (large)                                                                                               \
+      hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, 32, true>), grid, dim3(256), 0, stream, a);         \
+    else                                                                                                     \
+      hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, 4, false>), grid, dim3(256), 0, stream, a);         \
+  }
     ETA_PSUM(64, 64) ETA_PSUM(64, 128) ETA_PSUM(128, 64) ETA_PSUM(128, 128)
 #undef ETA_PSUM
   });

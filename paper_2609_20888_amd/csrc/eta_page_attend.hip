@@ -5,16 +5,18 @@
 //   partial of a split: m = a reference maximum, l = sum 2^(x_t - m), acc = sum 2^(x_t - m) s_v v_t,
 //   x_t = S~_t log2 e; the partials are merged as those of the contiguous caches are.
 //
-// A wavefront takes 64 tokens of a page at a time, on the matrix cores from end to end and
-// without LDS.  Scores: A = 16 keys x 32 dims (codes widened to bf16, exactly), B = 32 dims x 16
-// query heads (columns past the group's heads are zero), four tiles of 16 keys.  Row i of tile t
-// is token 16 (i / 4) + 4 t + i % 4, so that the result hands lane (column c, lane group g) the
-// 16 consecutive tokens 16 g .. 16 g + 15 of head c, which after the gate and the softmax are,
-// as they lie, the B operand of p.V: A = 16 dims x 32 tokens of V, B = 32 tokens x 16 heads.  V
-// lies by dimension in the page, so lane (dim, g) reads its 16 tokens with one 16-byte load, and
-// the result is the output's transpose, whose columns are heads again: the softmax state and the
-// rescaling stay in the lane.  The contraction runs in the order the loads give (any order does
-// that both operands share).
+// A wavefront takes a unit of 64 tokens of a page at a time, on the matrix cores from end to end
+// and without LDS.  Scores: A = 16 keys x 32 dims (codes widened to bf16, exactly), B = 32 dims x
+// 16 columns, four tiles of 16 keys.  Row i of tile t is token 16 (i / 4) + 4 t + i % 4, so that
+// the result hands lane (column, lane group g) the tokens 16 g + 4 t + r.  The columns repeat the
+// group's heads (column G j + h: head h), and replica j takes the gate and the softmax of its
+// share of the tiles alone, so that every lane has scores of its own to work on (one replica and
+// idle columns: four heads, 512K tokens, 71 -> us).  The weights are, as they lie, the B operand
+// of p.V, with zeros for the other replicas' tokens: A = 16 dims x 32 tokens of V, which lies by
+// dimension in the page, so that lane (dim, g) reads its 16 tokens with one 16-byte load.  The
+// result is the output's transpose, columns as before: the softmax state and the rescaling stay
+// in the lane, each replica has its own, and they are merged once at the end.  The contraction
+// runs in the order the loads give (any order does that both operands share).
 //
 // The weights go to p.V as two bf16 parts (16 bits), and fp32 queries as three with weights of
 // three: MFMA time is not what bounds these kernels.
@@ -25,6 +27,7 @@
 #include "eta_index.h"
 #include "eta_lanes.h"
 #include "eta_page.h"
+#include "eta_page_codes.h"
 
 namespace eta {
 
@@ -67,43 +70,27 @@ constexpr int kItems = 256;                  // 64-token units resolved at a tim
 constexpr uint32_t kIdMask = 0x00ffffffu;    // union id: block index | head bits << 24
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Eight codes -> eight bf16, exactly.
-__device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b) {
-  union {
-    bf16x2_t p[4];
-    bf16x8 v;
-  } u;
-  u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false);
-  u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-  u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
-  u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
-  return u.v;
-}
-
-// x in N bf16 parts, the largest first: each is the nearest to what the ones before it leave, so
-// N = 2 keep 16 bits of x and N = 3 all 24.
-template <int N>
-__device__ __forceinline__ void in_parts(const float (&x)[8], bf16x8 (&out)[N]) {
-  float r[8];
+// x in N bf16 parts, the largest first, as packed words: each part is the nearest to what the
+// ones before it leave, so N = 2 keep 16 bits of x and N = 3 all 24.
+template <int M, int N>
+__device__ __forceinline__ void in_parts(const float (&x)[M], uint32_t (&out)[N][M / 2]) {
+  float r[M];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = x[e];
+  for (int e = 0; e < M; ++e) r[e] = x[e];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    union {
-      uint32_t w[4];
-      bf16x8 v;
-    } u;
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) u.w[e / 2] = pack_bf16x2(r[e], r[e + 1]);
-    out[n] = u.v;
-    if (n + 1 < N) {
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        r[e] -= __uint_as_float(u.w[e / 2] << 16);
-        r[e + 1] -= __uint_as_float(u.w[e / 2] & 0xffff0000u);
+    for (int e = 0; e < M; e += 2) {
+      const uint32_t w = pack_bf16x2(r[e], r[e + 1]);
+      out[n][e / 2] = w;
+      if (n + 1 < N) {
+        r[e] -= __uint_as_float(w << 16);
+        r[e + 1] -= __uint_as_float(w & 0xffff0000u);
       }
     }
-  }
+}
+__device__ __forceinline__ bf16x8 as_bf16(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
 }
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
@@ -138,45 +125,41 @@ struct Column {
   f32x4 acc[D / 16];
 };
 
-// One unit of 64 tokens as its loads left it, with what the loop has to know of it.
-template <int D>
-struct Unit {
-  uint4 k[4][D / 64];
-  uint4 v[D / 16];
-};
-
-template <int D, bool DENSE, bool F32>
+template <int D, bool DENSE, bool F32, int REP>
 struct Attend {
   static constexpr int NQ = F32 ? 3 : 1;     // bf16 parts of the queries
   static constexpr int NP = F32 ? 3 : 2;     // and of the weights
   static constexpr int NC = D / 32;          // steps of a score's contraction
+  static constexpr int TS = 4 / REP;         // tiles of a replica
+  static constexpr int NS = 4 * TS;          // scores of a lane
   bf16x8 q[NC][NQ];
   float s2, beta, bt;                        // log2 e / sqrt d; gate exponent: bt - beta x
-  int lane;
+  int lane, rep;                             // rep: the lane's replica (REP and more: idle)
 
-  // This lane's share of the queries: column c's dims 64 h + 16 g + 8 e .. + 7 in step 2 h + e.
-  __device__ __forceinline__ void load_q(const PageSplitArgs& a, int64_t hq0, int G) {
-    const int col = lane & 15, g4 = lane >> 4;
-    const bool in = col < G;
-    const int64_t row = (hq0 + (in ? col : 0)) * D;
+  // This lane's share of the queries: head h's dims 64 k + 16 g + 8 e .. + 7 in step 2 k + e.
+  __device__ __forceinline__ void load_q(const PageSplitArgs& a, int64_t row) {
+    const int g4 = lane >> 4;
 #pragma unroll
     for (int s = 0; s < NC; ++s) {
       const int at = 64 * (s >> 1) + 16 * g4 + 8 * (s & 1);
       if constexpr (F32) {
         const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + row + at);
         const float4 u = p[0], w = p[1];
-        const float x[8] = {in ? u.x : 0.f, in ? u.y : 0.f, in ? u.z : 0.f, in ? u.w : 0.f,
-                            in ? w.x : 0.f, in ? w.y : 0.f, in ? w.z : 0.f, in ? w.w : 0.f};
-        in_parts<NQ>(x, q[s]);
+        const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+        uint32_t y[NQ][4];
+        in_parts<8, NQ>(x, y);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) q[s][n] = as_bf16(y[n][0], y[n][1], y[n][2], y[n][3]);
       } else {
-        uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + row + at);
-        if (!in) u = make_uint4(0u, 0u, 0u, 0u);
-        q[s][0] = __builtin_bit_cast(bf16x8, u);
+        q[s][0] = __builtin_bit_cast(
+            bf16x8, *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + row + at));
       }
     }
   }
 
-  __device__ __forceinline__ void scores(const Unit<D>& u, f32x4 (&c)[4]) const {
+  // The scores' products <q, c> of the lane's tokens.
+  __device__ __forceinline__ void scores(const uint4 (&k)[4][D / 64], float (&c)[NS]) const {
+    f32x4 all[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       f32x4 part[NQ];
@@ -184,33 +167,41 @@ struct Attend {
       for (int n = 0; n < NQ; ++n) part[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NC; ++s) {
-        const uint4& x = u.k[t][s >> 1];
+        const uint4& x = k[t][s >> 1];
         const bf16x8 kb = (s & 1) ? widen(x.z, x.w) : widen(x.x, x.y);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) part[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, q[s][n], part[n], 0, 0, 0);
       }
-      c[t] = part[NQ - 1];                   // the low parts' sums first
+      all[t] = part[NQ - 1];                 // the low parts' sums first
 #pragma unroll
-      for (int n = NQ - 2; n >= 0; --n) c[t] += part[n];
+      for (int n = NQ - 2; n >= 0; --n) all[t] += part[n];
+    }
+#pragma unroll
+    for (int e = 0; e < NS; ++e) {
+      const int i = e >> 2, r = e & 3;
+      if constexpr (REP == 4)
+        c[e] = rep < 2 ? (rep == 0 ? all[0][r] : all[1][r]) : (rep == 2 ? all[2][r] : all[3][r]);
+      else
+        c[e] = rep == 0 ? all[i][r] : all[2 + i][r];
     }
   }
 
   // Scores -> weights.  n: tokens of the unit that are there; on: whether the lane's head
   // attends it; self: the unit's token that is not gated (or none of 0..63).
-  __device__ __forceinline__ void weights(const f32x4 (&c)[4], int n, bool on, int self, float ks,
-                                          Column<D>& st, float (&p)[16]) const {
-    const int nl = on ? n - 16 * (lane >> 4) : 0, sl = self - 16 * (lane >> 4);
+  __device__ __forceinline__ void weights(const float (&c)[NS], int n, bool on, int self, float ks,
+                                          Column<D>& st, float (&p)[NS]) const {
+    const int tok = 16 * (lane >> 4) + NS * rep;
+    const int nl = on ? n - tok : 0, sl = self - tok;
     const float f = ks * s2;
-    float y[16], x[16];
+    float y[NS], x[NS];
     bool over = false;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float ce = c[e >> 2][e & 3];
-      y[e] = ce;
+    for (int e = 0; e < NS; ++e) {
+      y[e] = c[e];
       if constexpr (!DENSE) {
-        const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fmaf(-beta, ce * f, bt)));
+        const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fmaf(-beta, c[e] * f, bt)));
         // (an open gate passes any score, -inf too, where the gate's own sum is NaN)
-        y[e] = (e == sl || bt == kNegInf) ? ce : ce * sig;
+        y[e] = (e == sl || bt == kNegInf) ? c[e] : c[e] * sig;
       }
       x[e] = e < nl ? y[e] * f : kNegInf;
       over |= x[e] > st.t;
@@ -218,7 +209,7 @@ struct Attend {
     if (__ballot(over) != 0ull) {
       float bm = x[0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) bm = fmaxf(bm, x[e]);
+      for (int e = 1; e < NS; ++e) bm = fmaxf(bm, x[e]);
       bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
       bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
       const bool first = st.t == kNegInf;
@@ -231,25 +222,32 @@ struct Attend {
       for (int k = 0; k < D / 16; ++k) st.acc[k] *= alpha;
     }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < NS; ++e) {
       p[e] = e < nl ? __builtin_amdgcn_exp2f(fmaf(y[e], f, -st.m)) : 0.f;
       st.l += p[e];
     }
   }
 
-  __device__ __forceinline__ void values(const Unit<D>& u, const float (&p)[16], bool on, float vs,
+  __device__ __forceinline__ void values(const uint4 (&v)[D / 16], const float (&p)[NS], bool on, float vs,
                                          Column<D>& st) const {
+    uint32_t y[NP][NS / 2];
+    in_parts<NS, NP>(p, y);
     bf16x8 w[2][NP];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      float x[8];
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = p[8 * m + e];
-      in_parts<NP>(x, w[m]);
-    }
+      for (int n = 0; n < NP; ++n) {
+        if constexpr (REP == 4) {
+          const bool lo = rep == 2 * m, hi = rep == 2 * m + 1;
+          w[m][n] = as_bf16(lo ? y[n][0] : 0u, lo ? y[n][1] : 0u, hi ? y[n][0] : 0u, hi ? y[n][1] : 0u);
+        } else {
+          const bool in = rep == m;
+          w[m][n] = as_bf16(in ? y[n][0] : 0u, in ? y[n][1] : 0u, in ? y[n][2] : 0u, in ? y[n][3] : 0u);
+        }
+      }
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-      const bf16x8 v0 = widen(u.v[k].x, u.v[k].y), v1 = widen(u.v[k].z, u.v[k].w);
+      const bf16x8 v0 = widen(v[k].x, v[k].y), v1 = widen(v[k].z, v[k].w);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int n = NP - 1; n >= 0; --n) {
@@ -267,7 +265,7 @@ struct Attend {
 
 // Tokens from n on of a unit's values weigh 0, but what lies there may be NaN: made zero.
 template <int D>
-__device__ __forceinline__ void clear_behind(Unit<D>& u, int n, int lane) {
+__device__ __forceinline__ void clear_behind(uint4 (&v)[D / 16], int n, int lane) {
   const int nl = n - 16 * (lane >> 4);
   uint32_t keep[4];
 #pragma unroll
@@ -277,10 +275,10 @@ __device__ __forceinline__ void clear_behind(Unit<D>& u, int n, int lane) {
   }
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
-    u.v[k].x &= keep[0];
-    u.v[k].y &= keep[1];
-    u.v[k].z &= keep[2];
-    u.v[k].w &= keep[3];
+    v[k].x &= keep[0];
+    v[k].y &= keep[1];
+    v[k].z &= keep[2];
+    v[k].w &= keep[3];
   }
 }
 
@@ -291,27 +289,31 @@ __device__ __forceinline__ void store_o(void* o, int q_dtype, int64_t idx, float
     reinterpret_cast<__bf16*>(o)[idx] = (__bf16)x;
 }
 
-template <int D, bool DENSE, bool PROP, bool F32>
-__global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a) {
+template <int D, int BS, bool DENSE, bool PROP, bool F32, int REP>
+__global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_kernel(PageSplitArgs a) {
   constexpr int GPT = kPropMaxGroups / kThreads, CPT = kPropMaxCounts / kThreads;
   const Geom& g = a.pg.g;
-  const int G = g.G, BS = g.BS, tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
-  const int spb = BS >> 6, spb_log = BS >> 7;      // units of a block: 1 or 2
+  const int G = g.G, tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+  constexpr int spb = BS >> 6, spb_log = BS >> 7;  // units of a block: 1 or 2
   __shared__ int wsum_s[kWaves];
   __shared__ int pref_s[DENSE ? 1 : (PROP ? kPropMaxCounts : kMaxTiles) + 1];
   __shared__ int own_s[3];
   __shared__ int item_page[kItems];
   __shared__ uint32_t item_meta[kItems];           // head bits | sub << 8 | tokens << 16 | own token << 24
-  __shared__ float item_ks[kItems], item_vs[kItems];
-  __shared__ float mrg_ml[kWaves][kMaxGroup][2];
-  __shared__ __attribute__((aligned(16))) float mrg_acc[kWaves][kMaxGroup][D];
+  __shared__ float mrg_m[kWaves][16], mrg_l[kWaves][16];
+  __shared__ __attribute__((aligned(16))) float mrg_acc[kWaves][16][D];
+  __shared__ float rbest_s[DENSE ? 1 : kMaxGroup][kRescueTiles];
+  __shared__ int rinfo_s[DENSE ? 1 : kMaxGroup][kRescueTiles];
   __shared__ int resc_s[kMaxGroup], rxw_s[kMaxGroup], rx_s[kMaxGroup][2], nrx_s;
 
   // ---- which (sequence, kv head) and which split of it.  Uniform plan: grid (S, Hkv, B).
-  // Proportional plan (several sequences): a 1-D grid dealt to the groups by their units.
-  int b, gh, s, S, first, UI;
-  int pbase = 0;                     // the group's prefix within pref_s starts at pref0, offset by pbase
+  // Proportional plan (several sequences): a 1-D grid dealt to the groups by their units.  Loads
+  // that do not wait for each other are requested together: a step on its own is mostly their
+  // round trips.
+  int b, gh, s, S, first, UI, tc0 = 0;
+  int pbase = 0;                     // the group's tile prefix is pref[], offset by pbase
   const int* pref = pref_s;
+  const int32_t* tc = nullptr;
   if constexpr (!PROP) {
     s = blockIdx.x;
     gh = blockIdx.y;
@@ -319,29 +321,33 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
     S = gridDim.x;
     first = (b * g.Hkv + gh) * S;
     if constexpr (!DENSE) {
-      const int32_t* tc = a.tile_cnt + ((int64_t)b * g.Hkv + gh) * g.n_tiles;
-      int carry = 0;
-      for (int base = 0; base < g.n_tiles; base += kThreads) {
-        const int t = base + tid;
-        int tot;
-        const int ex = block_excl_scan(t < g.n_tiles ? tc[t] : 0, wsum_s, &tot);
-        if (t < g.n_tiles) pref_s[t] = carry + ex;
-        carry += tot;
-      }
-      if (tid == 0) pref_s[g.n_tiles] = carry;
-      UI = carry;
+      tc = a.tile_cnt + ((int64_t)b * g.Hkv + gh) * g.n_tiles;
+      tc0 = tid < g.n_tiles ? tc[tid] : 0;
     }
   } else {
     const int BG = g.B * g.Hkv, nct = g.n_tiles, nc = BG * nct, W = gridDim.x, me = blockIdx.x;
     if (tid == 0) own_s[0] = -1;
-    int work[GPT], tot;
+    int work[GPT], len[GPT], cv[CPT], tot;
     if constexpr (!DENSE) {
-      int cv[CPT], run = 0;
 #pragma unroll
       for (int k = 0; k < CPT; ++k) {
         const int i = tid * CPT + k;
         cv[k] = a.tile_cnt[i < nc ? i : 0];
       }
+    }
+    {
+      GroupStepper gs((unsigned)(tid * GPT), 1u, (unsigned)g.Hkv);
+#pragma unroll
+      for (int r = 0; r < GPT; ++r) {
+        len[r] = a.seq_lens[tid * GPT + r < BG ? gs.q : 0u];
+        gs.next();
+      }
+    }
+    // (all of them are needed here, so that none is moved into a branch)
+#pragma unroll
+    for (int r = 0; r < GPT; ++r) asm volatile("" ::"v"(len[r]));
+    if constexpr (!DENSE) {
+      int run = 0;
 #pragma unroll
       for (int k = 0; k < CPT; ++k) {
         const int x = tid * CPT + k < nc ? cv[k] : 0;
@@ -356,18 +362,16 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
     }
     // the groups' units (thread tid: groups GPT tid ..), and splits in proportion to them
     int mine = 0;
-    GroupStepper gs((unsigned)(tid * GPT), 1u, (unsigned)g.Hkv);
 #pragma unroll
     for (int r = 0; r < GPT; ++r) {
       const int x = tid * GPT + r;
       work[r] = 0;
       if (x < BG) {
-        const int64_t len = clamp_len(a.seq_lens, (int)gs.q, g.cap);
-        const int blocks = DENSE ? (int)(len / BS) : pref_s[(x + 1) * nct] - pref_s[x * nct];
-        work[r] = group_work(blocks, spb, len, BS);
+        const int64_t t = len[r] < 0 ? 0 : (len[r] > g.cap ? g.cap : len[r]);
+        const int blocks = DENSE ? (int)(t / BS) : pref_s[(x + 1) * nct] - pref_s[x * nct];
+        work[r] = group_work(blocks, spb, t, BS);
       }
       mine += work[r];
-      gs.next();
     }
     block_excl_scan(mine, wsum_s, &tot);
     int nsp[GPT], sum = 0, dummy;
@@ -403,38 +407,69 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
   }
   const int64_t hq0 = (int64_t)b * g.Hq + (int64_t)gh * G, bg = (int64_t)b * g.Hkv + gh;
   const bool single = !PROP && S == 1;             // no partials, no combine
-  const int64_t T = clamp_len(a.seq_lens, b, g.cap);
-  const int64_t N = T / BS;
-  const int ntail = (int)(T - N * BS);
-  if constexpr (DENSE) UI = (int)N;
-
-  Attend<D, DENSE, F32> at;
+  const int col = lane & 15, head = col % G;       // (G divides 16)
+  Attend<D, DENSE, F32, REP> at;
   at.lane = lane;
+  at.rep = col / G;
   at.s2 = kLog2e / sqrtf((float)D);
   at.beta = a.beta;
   at.bt = kNegInf;
-  at.load_q(a, hq0, G);
-  const int col = lane & 15;
+  int t_raw = a.seq_lens[b];
+  float tau = 0.f, rb = 0.f;
+  int ri = 0;
   if constexpr (!DENSE) {
-    const float teff = (col < G ? a.tau[hq0 + col] : 0.f) - a.offset_a;
+    tau = a.tau[hq0 + head];
+    // (the parts of every window tile: those past the window are not used)
+    const int64_t e = hq0 * kRescueTiles + (tid < G * kRescueTiles ? tid : 0);
+    rb = a.resc_best[e];
+    ri = a.resc_info[e];
+  }
+  at.load_q(a, (hq0 + head) * D);
+  asm volatile("" : "+v"(t_raw) : "v"(tau), "v"(rb), "v"(ri), "v"(tc0));
+  t_raw = __builtin_amdgcn_readfirstlane(t_raw);
+  const int64_t T = t_raw < 0 ? 0 : (t_raw > g.cap ? g.cap : (int64_t)t_raw);
+  const int64_t N = T / BS;
+  const int ntail = (int)(T - N * BS);
+  if constexpr (DENSE) UI = (int)N;
+  if constexpr (!DENSE) {
+    const float teff = tau - a.offset_a;
     at.bt = teff == kNegInf ? kNegInf : a.beta * teff * kLog2e;
+    if (tid < G * kRescueTiles) {
+      rbest_s[tid / kRescueTiles][tid % kRescueTiles] = rb;
+      rinfo_s[tid / kRescueTiles][tid % kRescueTiles] = ri;
+    }
+    if constexpr (!PROP) {
+      int carry = 0;
+      for (int base = 0; base < g.n_tiles; base += kThreads) {
+        const int t = base + tid;
+        int tot;
+        const int ex = block_excl_scan(base == 0 ? tc0 : (t < g.n_tiles ? tc[t] : 0), wsum_s, &tot);
+        if (t < g.n_tiles) pref_s[t] = carry + ex;
+        carry += tot;
+      }
+      if (tid == 0) {
+        pref_s[g.n_tiles] = carry;
+        if (s == 0) a.plan[bg] = make_int2(first, S);
+      }
+      UI = carry;
+    }
+    __syncthreads();
   }
 
   // ---- top-1 rescue: for each head, when no block of the window is selected, the first of the
   // window's largest bounds (tiles in order) is attended too; each distinct one is a further item
   // of the list, with the heads that rescued it
-  int jr_h = -1, wb_rescued = 1;
+  int jr_h = -1, wb_rescued = 1, nrx = 0;
   const int UI_union = UI;
   if constexpr (!DENSE) {
     const int64_t Wn = (int64_t)a.c < N ? (int64_t)a.c : N;
     const int nwt = (int)((Wn + kScreenTile - 1) / kScreenTile);
-    if (tid < G) {
+    if (lane < G) {                  // (every wavefront, so that all know whether there is any)
       float best = kNegInf;
       bool any = false;
       for (int t = 0; t < nwt; ++t) {
-        const int64_t e = (hq0 + tid) * kRescueTiles + t;
-        const int inf = a.resc_info[e];
-        const float v = a.resc_best[e];
+        const int inf = rinfo_s[lane][t];
+        const float v = rbest_s[lane][t];
         if (inf == kRescueAny) {
           any = true;
         } else if (inf >= 0 && (jr_h < 0 || v > best)) {
@@ -443,49 +478,53 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
         }
       }
       if (any) jr_h = -1;
-      resc_s[tid] = jr_h;
-      if (s == S - 1 && jr_h >= 0) wb_rescued = a.wbits[bg * kMaxRescueWindow + jr_h];
     }
-    if (!PROP && s == 0 && tid == 0) a.plan[bg] = make_int2(first, S);
-    __syncthreads();
-    if (tid == 0) {
-      int nb = 0;
-      for (int h = 0; h < G; ++h) {
-        const int j = resc_s[h];
-        if (j < 0) continue;
-        int k = 0;
-        while (k < nb && rx_s[k][0] != j) ++k;
-        if (k == nb) {
-          rx_s[nb][0] = j;
-          rx_s[nb][1] = 0;
-          ++nb;
-        }
-        rx_s[k][1] |= 1 << h;
+    if (__ballot(jr_h >= 0) != 0ull) {
+      if (tid < G) {
+        resc_s[tid] = jr_h;
+        if (s == S - 1 && jr_h >= 0) wb_rescued = a.wbits[bg * kMaxRescueWindow + jr_h];
       }
-      nrx_s = nb;
+      __syncthreads();
+      if (tid == 0) {
+        int nb = 0;
+        for (int h = 0; h < G; ++h) {
+          const int j = resc_s[h];
+          if (j < 0) continue;
+          int k = 0;
+          while (k < nb && rx_s[k][0] != j) ++k;
+          if (k == nb) {
+            rx_s[nb][0] = j;
+            rx_s[nb][1] = 0;
+            ++nb;
+          }
+          rx_s[k][1] |= 1 << h;
+        }
+        nrx_s = nb;
+      }
+      __syncthreads();
+      nrx = nrx_s;
+      UI += nrx;
     }
-    __syncthreads();
-    UI += nrx_s;
   }
 
-  // ---- the list's units: the items' blocks, then the tail; this split has units s, s + S, ...
+  // ---- the list: its items' blocks, then the tail.  This split has items s, s + S, ..; the units
+  // of an item are neighbours, so that the wavefronts that take them read the halves of V's lines
+  // (blocks of 128 tokens) at about the same time
   const uint32_t all_bits = (1u << G) - 1u;
-  const int64_t units = (int64_t)UI * spb, total = units + (ntail + 63) / 64;
+  const int total = UI + (ntail > 0);
   const int64_t self_t = (!DENSE && a.self_ungated) ? T - 1 : -1;
   const int32_t* row = a.table + (int64_t)b * a.pg.table_stride;
-  auto resolve = [&](int64_t t, int slot) {
-    int64_t j = N;
-    int sub, n = 64;
+  auto resolve = [&](int unit, int slot) {
+    const int it = s + S * (unit >> spb_log), sub = unit & (spb - 1);
+    int64_t j = it;
+    int n = 64;
     uint32_t bits = all_bits;
-    if (t >= units) {
-      sub = (int)(t - units);
-      n = ntail - 64 * sub < 64 ? ntail - 64 * sub : 64;
-    } else {
-      const int it = (int)(t >> spb_log);
-      sub = (int)(t & (spb - 1));
-      if constexpr (DENSE) {
-        j = it;
-      } else if (it >= UI_union) {
+    if (it >= UI) {
+      j = N;
+      n = ntail - 64 * sub;
+      n = n < 0 ? 0 : (n > 64 ? 64 : n);
+    } else if constexpr (!DENSE) {
+      if (it >= UI_union) {
         j = rx_s[it - UI_union][0];
         bits = (uint32_t)rx_s[it - UI_union][1];
       } else {
@@ -504,8 +543,6 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
     const int64_t own = self_t - (j * BS + 64 * sub);
     item_page[slot] = (int)page;
     item_meta[slot] = bits | (uint32_t)sub << 8 | (uint32_t)n << 16 | (own >= 0 && own < 64 ? (uint32_t)own : 255u) << 24;
-    item_ks[slot] = a.k_scale[page * a.pg.scale_stride + gh];
-    item_vs[slot] = a.v_scale[page * a.pg.scale_stride + gh];
   };
 
   Column<D> st;
@@ -514,67 +551,74 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) st.acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int ri = lane & 15, g4 = lane >> 4;
+  const int g4 = lane >> 4;
   const int64_t head_off = (int64_t)gh * BS * D;
-  const uint8_t* kl = a.k + head_off + (16 * (ri >> 2) + (ri & 3)) * D + 16 * g4;
-  const uint8_t* vl = a.v + head_off + ri * BS + 16 * g4;
-  Unit<D> u;
-  auto unit_of = [&](int x, int64_t* koff, int64_t* voff) {
-    const int64_t page = __builtin_amdgcn_readfirstlane(item_page[x]);
-    const int sub = (__builtin_amdgcn_readfirstlane(item_meta[x]) >> 8) & 255;
-    *koff = page * a.pg.page_stride + sub * 64 * D;
-    *voff = page * a.pg.page_stride + sub * 64;
-  };
+  const uint8_t* kl = a.k + head_off + (16 * (col >> 2) + (col & 3)) * D + 16 * g4;
+  const uint8_t* vl = a.v + head_off + col * BS + 16 * g4;
+  uint4 kr[4][D / 64], vr[D / 16];
   auto load_k = [&](int64_t off) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int h = 0; h < D / 64; ++h) u.k[t][h] = load16(kl + off + 4 * t * D + 64 * h);
+      for (int h = 0; h < D / 64; ++h) kr[t][h] = load16(kl + off + 4 * t * D + 64 * h);
   };
+  // (a block's 64 tokens of a row of V: whole lines, read once, past the caches; halves of the
+  // lines of 128 tokens, whose other halves a neighbour reads, through them)
   auto load_v = [&](int64_t off) {
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) u.v[k] = load16_nt(vl + off + 16 * k * BS);
+    for (int k = 0; k < D / 16; ++k) {
+      if constexpr (BS == 64)
+        vr[k] = load16_nt(vl + off + 16 * k * BS);
+      else
+        vr[k] = load16(vl + off + 16 * k * BS);
+    }
   };
-  auto tile = [&](int x, int64_t kn, int64_t vn, auto more_tag) {
-    constexpr bool MORE = decltype(more_tag)::value;
+  // The unit that is worked on and the next one: page, part of the block, the page's scales (which
+  // come while its keys do).
+  int64_t at_n = 0;                  // the next unit's page
+  int sub_n = 0;
+  float ks_n = 0.f, vs_n = 0.f;
+  auto next = [&](int x) {
+    at_n = __builtin_amdgcn_readfirstlane(item_page[x]);
+    sub_n = (__builtin_amdgcn_readfirstlane(item_meta[x]) >> 8) & 255;
+    ks_n = a.k_scale[at_n * a.pg.scale_stride + gh];
+    vs_n = a.v_scale[at_n * a.pg.scale_stride + gh];
+  };
+  // The next unit's keys are requested as soon as this one's scores have taken theirs, its values
+  // when p.V has.  The last unit is peeled (more false), so that the loads in the loop are
+  // unconditional.
+  auto unit = [&](int x, auto more_tag) {
+    constexpr bool more = decltype(more_tag)::value;
     const uint32_t meta = __builtin_amdgcn_readfirstlane(item_meta[x]);
-    const float ks = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(item_ks[x])));
-    const float vs = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(item_vs[x])));
+    const float ks = ks_n, vs = vs_n;
     const int n = (meta >> 16) & 255;
-    const bool on = (meta >> col) & 1u & (col < G);
-    f32x4 c[4];
-    at.scores(u, c);
-    if constexpr (MORE) {
-      __builtin_amdgcn_sched_barrier(0);
-      load_k(kn);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    float p[16];
+    const bool on = at.rep < REP && ((meta >> head) & 1u);
+    constexpr int NS = Attend<D, DENSE, F32, REP>::NS;
+    float c[NS], p[NS];
+    if constexpr (more) next(x + kWaves);
+    at.scores(kr, c);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (more) load_k(at_n * a.pg.page_stride + sub_n * 64 * D);
+    __builtin_amdgcn_sched_barrier(0);
     at.weights(c, n, on, (int)(meta >> 24), ks, st, p);
-    if (n < 64) clear_behind<D>(u, n, lane);
-    at.values(u, p, on, vs, st);
-    if constexpr (MORE) {
-      __builtin_amdgcn_sched_barrier(0);
-      load_v(vn);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    if (n < 64) clear_behind<D>(vr, n, lane);
+    at.values(vr, p, on, vs, st);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (more) load_v(at_n * a.pg.page_stride + sub_n * 64);
+    __builtin_amdgcn_sched_barrier(0);
   };
-  const int nt = strided_share(total, s, S);
+  const int nt = strided_share(total, s, S) * spb;
   for (int k0 = 0; k0 < nt; k0 += kItems) {
     const int n = nt - k0 < kItems ? nt - k0 : kItems;
-    if (tid < n) resolve(s + (int64_t)S * (k0 + tid), tid);
+    if (tid < n) resolve(k0 + tid, tid);
     __syncthreads();
     if (w < n) {
-      int64_t ko, vo;
-      unit_of(w, &ko, &vo);
-      load_k(ko);
-      load_v(vo);
+      next(w);
+      load_k(at_n * a.pg.page_stride + sub_n * 64 * D);
+      load_v(at_n * a.pg.page_stride + sub_n * 64);
       int x = w;
-      for (; x + kWaves < n; x += kWaves) {
-        unit_of(x + kWaves, &ko, &vo);
-        tile(x, ko, vo, std::integral_constant<bool, true>{});
-      }
-      tile(x, 0, 0, std::integral_constant<bool, false>{});
+      for (; x + kWaves < n; x += kWaves) unit(x, std::integral_constant<bool, true>{});
+      unit(x, std::integral_constant<bool, false>{});
     }
     __syncthreads();
   }
@@ -582,59 +626,67 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
   if constexpr (!DENSE) {
     if (s == S - 1) {
       // the rescued blocks' mask bits; each head's rescued block and how many are outside the union
-      if (tid < G) rxw_s[tid] = jr_h >= 0 ? wb_rescued : 1;
-      __syncthreads();
-      if (tid == 0) {
-        int extra = 0;
-        for (int k = 0; k < nrx_s; ++k) {
+      int extra = 0;
+      if (nrx > 0) {
+        if (tid < G) rxw_s[tid] = jr_h >= 0 ? wb_rescued : 1;
+        __syncthreads();
+        for (int k = 0; k < nrx; ++k) {
           bool in_union = false;
           for (int h = 0; h < G; ++h) in_union |= resc_s[h] == rx_s[k][0] && rxw_s[h] != 0;
           extra += !in_union;
         }
+        if (tid < G && jr_h >= 0) a.mask[(hq0 + tid) * g.ncap + jr_h] = 1;
+      }
+      if (tid == 0) {
         if (!single)
           a.extra_union[bg] = extra;
         else if (a.union_counts != nullptr)
           a.union_counts[bg] = UI_union + extra;
       }
-      if (tid < G) {
-        if (!single) a.resc_out[hq0 + tid] = jr_h;
-        if (jr_h >= 0) a.mask[(hq0 + tid) * g.ncap + jr_h] = 1;
-      }
+      if (!single && tid < G) a.resc_out[hq0 + tid] = jr_h;
     }
   }
 
-  // ---- merge of the four wavefronts
+  // ---- merge of the wavefronts' replicas
   st.l += __shfl_xor(st.l, 16, 64);
   st.l += __shfl_xor(st.l, 32, 64);
-  if (col < G) {
-    if (g4 == 0) {
-      mrg_ml[w][col][0] = st.t == kNegInf ? kNegInf : st.m;
-      mrg_ml[w][col][1] = st.l;
-    }
+  if (g4 == 0) {
+    mrg_m[w][col] = st.t == kNegInf ? kNegInf : st.m;          // (idle columns: none)
+    mrg_l[w][col] = st.l;
+  }
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) *reinterpret_cast<f32x4*>(&mrg_acc[w][col][16 * k + 4 * g4]) = st.acc[k];
+  for (int k = 0; k < D / 16; ++k) *reinterpret_cast<f32x4*>(&mrg_acc[w][col][16 * k + 4 * g4]) = st.acc[k];
+  __syncthreads();
+  // wavefront 0, lane (w', column): the weight of that replica, the head's maximum and sum
+  float ms = kNegInf;
+  if (w == 0) {
+    const float mk = mrg_m[lane >> 4][col];
+    ms = mk;
+    for (int o = G; o < 16; o <<= 1) ms = fmaxf(ms, __shfl_xor(ms, o, 64));
+    ms = fmaxf(ms, __shfl_xor(ms, 16, 64));
+    ms = fmaxf(ms, __shfl_xor(ms, 32, 64));
+    const float wk = mk == kNegInf ? 0.f : __builtin_amdgcn_exp2f(mk - ms);
+    float L = mk == kNegInf ? 0.f : wk * mrg_l[lane >> 4][col];
+    for (int o = G; o < 64; o <<= 1) L += __shfl_xor(L, o, 64);
+    mrg_m[lane >> 4][col] = wk;
+    if (lane < G) {
+      mrg_l[0][lane] = L;
+      if (!single) a.part_ml[(int64_t)(first + s) * G + lane] = make_float2(ms, L);
+    }
   }
   __syncthreads();
   for (int idx = tid; idx < G * D; idx += kThreads) {
     const int h = idx / D, i = idx % D;
-    float ms = kNegInf;
+    float o = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) ms = fmaxf(ms, mrg_ml[k][h][0]);
-    float L = 0.f, o = 0.f;
+    for (int k = 0; k < kWaves; ++k)
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      const float mk = mrg_ml[k][h][0];
-      if (mk == kNegInf) continue;
-      const float wk = __builtin_amdgcn_exp2f(mk - ms);
-      L = fmaf(mrg_ml[k][h][1], wk, L);
-      o = fmaf(mrg_acc[k][h][i], wk, o);
-    }
+      for (int j = 0; j < REP; ++j) o = fmaf(mrg_acc[k][j * G + h][i], mrg_m[k][j * G + h], o);
     if (single) {
-      store_o(a.out, a.q_dtype, (hq0 + h) * D + i, ms == kNegInf ? 0.f : o / L);
+      const float L = mrg_l[0][h];
+      store_o(a.out, a.q_dtype, (hq0 + h) * D + i, L == 0.f ? 0.f : o / L);
     } else {
-      const int64_t pidx = (int64_t)(first + s) * G + h;
-      a.part_acc[pidx * D + i] = o;
-      if (i == 0) a.part_ml[pidx] = make_float2(ms, L);
+      a.part_acc[((int64_t)(first + s) * G + h) * D + i] = o;
     }
   }
   if constexpr (!DENSE) {
@@ -644,7 +696,7 @@ __global__ __launch_bounds__(kThreads, 2) void page_split_kernel(PageSplitArgs a
         for (int t = lane; t < g.n_tiles; t += 64) cnt += a.head_cnt[(hq0 + h) * g.n_tiles + t];
 #pragma unroll
         for (int o2 = 32; o2 > 0; o2 >>= 1) cnt += __shfl_xor(cnt, o2, 64);
-        if (lane == 0) a.counts[hq0 + h] = (int32_t)(((int64_t)cnt + (resc_s[h] >= 0 ? 1 : 0)) * BS + ntail);
+        if (lane == 0) a.counts[hq0 + h] = (int32_t)(((int64_t)cnt + (nrx > 0 && resc_s[h] >= 0 ? 1 : 0)) * BS + ntail);
       }
     }
   }
@@ -654,11 +706,18 @@ template <bool DENSE>
 void launch_split(const PageSplitArgs& a, const SplitPlan& pl, hipStream_t stream) {
   const Geom& g = a.pg.g;
   const dim3 grid = pl.S > 0 ? dim3(pl.S, g.Hkv, g.B) : dim3(pl.W);
-#define ETA_PSPL(D_, P_, F_)                                                                             \
-  if (g.D == D_ && (pl.S == 0) == P_ && (a.q_dtype == ETA_DT_F32) == F_)                                 \
-    hipLaunchKernelGGL((page_split_kernel<D_, DENSE, P_, F_>), grid, dim3(kThreads), 0, stream, a);
-  ETA_PSPL(64, false, false) ETA_PSPL(64, false, true) ETA_PSPL(64, true, false) ETA_PSPL(64, true, true)
-  ETA_PSPL(128, false, false) ETA_PSPL(128, false, true) ETA_PSPL(128, true, false) ETA_PSPL(128, true, true)
+#define ETA_PSPL(D_, BS_, P_, F_)                                                                               \
+  if (g.D == D_ && g.BS == BS_ && (pl.S == 0) == P_ && (a.q_dtype == ETA_DT_F32) == F_) {                     \
+    if (g.G == 8)                                                                                             \
+      hipLaunchKernelGGL((page_split_kernel<D_, BS_, DENSE, P_, F_, 2>), grid, dim3(kThreads), 0, stream, a); \
+    else                                                                                                      \
+      hipLaunchKernelGGL((page_split_kernel<D_, BS_, DENSE, P_, F_, 4>), grid, dim3(kThreads), 0, stream, a); \
+  }
+#define ETA_PSPL_P(D_, BS_)                                           \
+  ETA_PSPL(D_, BS_, false, false) ETA_PSPL(D_, BS_, false, true)      \
+  ETA_PSPL(D_, BS_, true, false) ETA_PSPL(D_, BS_, true, true)
+  ETA_PSPL_P(64, 64) ETA_PSPL_P(64, 128) ETA_PSPL_P(128, 64) ETA_PSPL_P(128, 128)
+#undef ETA_PSPL_P
 #undef ETA_PSPL
 }
 
