@@ -194,6 +194,80 @@ __global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs 
   }
 }
 
+// One token of each sequence: one workgroup for a head of K or of V, every wavefront with the
+// token's row (a lane D / 64 of its values), so that its scale needs no exchange.  Where the page's
+// scale grows, the workgroup rounds the codes held again; else it writes the row.  All latency:
+// three round trips (start, table and row, scale).  32 sequences, 8 kv heads, d = 128: 7.2 us with
+// the kernel above, this one.
+template <int D, int BS, typename T>
+__global__ __launch_bounds__(256) void page_token_kernel(StoreArgs a) {
+  constexpr int PL = D / 64;
+  const int kv = blockIdx.x & 1, h = blockIdx.x >> 1, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const T* src = reinterpret_cast<const T*>(a.rows[kv]) + b * a.sb[kv] + h * a.sh[kv] + lane * PL;
+  float x[PL];
+#pragma unroll
+  for (int e = 0; e < PL; ++e) {
+    if constexpr (sizeof(T) == 4)
+      x[e] = src[e];
+    else
+      x[e] = __uint_as_float((uint32_t)src[e] << 16);
+  }
+  int64_t first, end;
+  new_span(a, b, &first, &end);
+  if (end <= first) return;
+  const int64_t j = first / BS, page = page_of(a.table + (int64_t)b * a.pg.table_stride, j, a.pg.table_blocks, a.pg.pages);
+  if (page < 0) return;
+  const int lo = (int)(first - j * BS);
+  const int64_t si = page * a.pg.scale_stride + h;
+  const float held = a.scale[kv][si];
+  uint8_t* dst = a.code[kv] + page * a.pg.page_stride + (int64_t)h * BS * D;
+  float amax = 0.f;
+#pragma unroll
+  for (int e = 0; e < PL; ++e) amax = fmaxf(amax, finite_abs(x[e]));
+  const int e2 = scale_exponent(wave_max64(amax));
+  const float need = power_of_two(e2);
+  const bool grows = lo == 0 || need > held;
+  const float inv = grows ? power_of_two(-e2) : 1.0f / held;
+  if (lo > 0 && grows) {
+    const float again = held / need;
+    for (int k = tid; k < BS * D / 16; k += 256) {
+      uint4* p = reinterpret_cast<uint4*>(dst) + k;
+      if (kv == 0) {
+        if (k >= lo * (D / 16)) break;
+        uint4 w = *p;
+        *p = make_uint4(scaled4(w.x, again), scaled4(w.y, again), scaled4(w.z, again), scaled4(w.w, again));
+      } else {
+        const int t0 = 16 * (k % (BS / 16));         // tokens t0 .. of a dimension
+        if (t0 >= lo) continue;
+        const uint4 v = *p;
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int nv = lo - t0 - 4 * i;              // tokens of the word that are held
+          const uint32_t m = nv >= 4 ? ~0u : (nv <= 0 ? 0u : (1u << (8 * nv)) - 1u);
+          w[i] = (scaled4(w[i], again) & m) | (w[i] & ~m);
+        }
+        *p = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    // (the words of V rounded again hold the new token's place)
+    __threadfence_block();
+    __syncthreads();
+  }
+  if (tid >= 64) return;
+  if (grows && lane == 0) a.scale[kv][si] = need;
+  const uint32_t w = pack4(coded(x[0], inv), coded(x[PL - 1], inv), 0.f, 0.f);
+  if (kv == 0) {
+    if constexpr (PL == 2)
+      reinterpret_cast<uint16_t*>(dst + lo * D)[lane] = (uint16_t)w;
+    else
+      dst[lo * D + lane] = (uint8_t)w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < PL; ++e) dst[(lane * PL + e) * BS + lo] = (uint8_t)(w >> (8 * e));
+  }
+}
+
 // ---------------------------------------------------------------- the index
 //
 // mu = s m, sigma = s sqrt(mean((c - m)^2)), M = s max |c_t| over the codes c of a block, m their
@@ -413,6 +487,8 @@ __global__ __launch_bounds__(256) void page_copy_kernel(eta_page_pool_t pool, Pa
 // the order of the free pages runs in one workgroup, which reads refs 4096 pages at a time.
 
 constexpr int kTableThreads = 1024;
+// Entries and counts up to which one workgroup goes over the table too: a launch less.
+constexpr int64_t kOneWorkgroup = 16384;
 
 // Exclusive prefix over the workgroup's kTableThreads threads; *total gets the sum.
 __device__ __forceinline__ int wide_excl_scan(int x, int* wsum, int* total) {
@@ -565,11 +641,10 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(eta_table_desc_t td, con
   }
 }
 
-__global__ __launch_bounds__(kTableThreads) void fork_pages_kernel(eta_table_desc_t td, const int32_t* seq_lens_out,
-                                                                   int32_t* table_out, int32_t* refs_out, int32_t* src,
-                                                                   int32_t* dst, int32_t* missing,
-                                                                   const int32_t* need, int32_t* free_list) {
-  __shared__ int wsum[kTableThreads / 64];
+// Gives the rows that copy a page their new one (one workgroup).
+__device__ __forceinline__ void fork_pages(const eta_table_desc_t& td, const int32_t* seq_lens_out, int32_t* table_out,
+                                           int32_t* refs_out, int32_t* src, int32_t* dst, int32_t* missing,
+                                           const int32_t* need, int32_t* free_list, int* wsum) {
   const int tid = threadIdx.x;
   int64_t want = 0;
   for (int base = 0; base < td.batch; base += kTableThreads) {
@@ -577,7 +652,10 @@ __global__ __launch_bounds__(kTableThreads) void fork_pages_kernel(eta_table_des
     wide_excl_scan(base + tid < td.batch && need[base + tid] >= 0, wsum, &tot);
     want += tot;
   }
-  const int64_t found = ranked(td.num_pages, want, wsum, [&](int64_t p) { return refs_out[p] <= 0; },
+  const int64_t found = ranked(td.num_pages, want, wsum, [&](int64_t p) {
+                                 // (atomics changed the counts past this compute unit's cache)
+                                 return __hip_atomic_load(refs_out + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) <= 0;
+                               },
                                [&](int64_t r, int64_t p) { free_list[r] = (int32_t)p; });
   const int64_t have = found < want ? found : want;
   if (tid == 0) missing[0] = (int32_t)(want - have);
@@ -605,10 +683,73 @@ __global__ __launch_bounds__(kTableThreads) void fork_pages_kernel(eta_table_des
   }
 }
 
+__global__ __launch_bounds__(kTableThreads) void fork_pages_kernel(eta_table_desc_t td, const int32_t* seq_lens_out,
+                                                                   int32_t* table_out, int32_t* refs_out, int32_t* src,
+                                                                   int32_t* dst, int32_t* missing,
+                                                                   const int32_t* need, int32_t* free_list) {
+  __shared__ int wsum[kTableThreads / 64];
+  fork_pages(td, seq_lens_out, table_out, refs_out, src, dst, missing, need, free_list, wsum);
+}
+
+// The whole of it in one workgroup, for tables of at most kTableThreads rows and few entries.
+__global__ __launch_bounds__(kTableThreads) void fork_kernel(eta_table_desc_t td, const int32_t* table,
+                                                             const int32_t* refs, const int32_t* seq_lens,
+                                                             const int32_t* parents, int32_t* table_out,
+                                                             int32_t* refs_out, int32_t* seq_lens_out, int32_t* src,
+                                                             int32_t* dst, int32_t* missing, int32_t* need,
+                                                             int32_t* free_list) {
+  __shared__ int wsum[kTableThreads / 64];
+  __shared__ int parent_s[kTableThreads], blocks_s[kTableThreads], copy_s[kTableThreads];
+  const int tid = threadIdx.x;
+  int a = -1;
+  int64_t full = 0, nb = 0;
+  if (tid < td.batch) {
+    a = parents[tid];
+    if (a < 0 || a >= td.batch) a = -1;
+    const int64_t cap = td.table_blocks * td.block_size;
+    int64_t len = a >= 0 ? seq_lens[a] : 0;
+    len = len < 0 ? 0 : (len > cap ? cap : len);
+    nb = blocks_of(td, len, &full);
+    seq_lens_out[tid] = (int32_t)len;
+    parent_s[tid] = a;
+    blocks_s[tid] = (int)nb;
+  }
+  for (int64_t p = tid; p < td.num_pages; p += kTableThreads) refs_out[p] = refs[p];
+  __threadfence_block();
+  __syncthreads();
+  if (tid < td.batch) {
+    bool copies = false;
+    if (full < nb)                   // whether an earlier row takes the last block already
+      for (int o = 0; o < tid; ++o) copies |= parent_s[o] == a;
+    copy_s[tid] = copies ? (int)full : -1;
+    const int32_t p = copies ? table[a * td.table_stride + full] : -1;
+    need[tid] = p >= 0 && p < td.num_pages ? p : -1;
+  }
+  __threadfence_block();
+  __syncthreads();
+  const int64_t entries = td.batch * td.table_blocks;
+  for (int64_t e = tid; e < entries; e += kTableThreads) {
+    const int b = (int)((uint32_t)e / (uint32_t)td.table_blocks);
+    const int64_t j = e - b * td.table_blocks;
+    const int32_t old = table[b * td.table_stride + j];
+    int32_t now = j < blocks_s[b] && j != copy_s[b] ? table[parent_s[b] * td.table_stride + j] : -1;
+    if (now < 0 || now >= td.num_pages) now = -1;
+    table_out[b * td.table_stride + j] = now;
+    if (old != now) {
+      if (old >= 0 && old < td.num_pages) atomicSub(refs_out + old, 1);
+      if (now >= 0) atomicAdd(refs_out + now, 1);
+    }
+  }
+  __threadfence_block();
+  __syncthreads();
+  fork_pages(td, seq_lens_out, table_out, refs_out, src, dst, missing, need, free_list, wsum);
+}
+
 // New numbers of the pages (map: -1 for free ones), the counts by them, and the pairs to copy.
 __global__ __launch_bounds__(kTableThreads) void compact_kernel(eta_table_desc_t td, const int32_t* refs,
                                                                 int32_t* refs_out, int32_t* src, int32_t* dst,
-                                                                int32_t* live, int32_t* map) {
+                                                                int32_t* live, int32_t* map, const int32_t* table,
+                                                                int32_t* table_out) {
   __shared__ int wsum[kTableThreads / 64];
   const int tid = threadIdx.x;
   const int64_t P = td.num_pages;
@@ -638,6 +779,16 @@ __global__ __launch_bounds__(kTableThreads) void compact_kernel(eta_table_desc_t
     if (p >= n) refs_out[p] = 0;
   }
   for (int64_t r = moves + tid; r < P / 2; r += kTableThreads) src[r] = dst[r] = -1;
+  if (table == nullptr) return;      // (its launch of its own follows)
+  __threadfence_block();
+  __syncthreads();
+  const int64_t entries = td.batch * td.table_blocks;
+  for (int64_t e = tid; e < entries; e += kTableThreads) {
+    const int b = (int)((uint32_t)e / (uint32_t)td.table_blocks);
+    const int64_t at = b * td.table_stride + (e - b * td.table_blocks);
+    const int32_t p = table[at];
+    table_out[at] = p >= 0 && p < P ? map[p] : -1;
+  }
 }
 
 __global__ __launch_bounds__(256) void compact_table_kernel(eta_table_desc_t td, const int32_t* table,
@@ -651,6 +802,14 @@ __global__ __launch_bounds__(256) void compact_table_kernel(eta_table_desc_t td,
 template <int D, int BS>
 void launch_store(const StoreArgs& a, bool f32, dim3 grid, hipStream_t stream) {
   const dim3 threads(D / 8 * (BS / 4));
+  if (a.new_tokens == 1) {
+    const Geom& g = a.pg.g;
+    if (f32)
+      hipLaunchKernelGGL((page_token_kernel<D, BS, float>), dim3(2 * g.Hkv, g.B), dim3(256), 0, stream, a);
+    else
+      hipLaunchKernelGGL((page_token_kernel<D, BS, uint16_t>), dim3(2 * g.Hkv, g.B), dim3(256), 0, stream, a);
+    return;
+  }
   if (f32)
     hipLaunchKernelGGL((page_store_kernel<D, BS, float>), grid, threads, 0, stream, a);
   else
@@ -733,6 +892,11 @@ hipError_t launch_page_fork(const eta_table_desc_t& td, const int32_t* table, co
                             const int32_t* seq_lens, const int32_t* parents, int32_t* table_out,
                             int32_t* refs_out, int32_t* seq_lens_out, int32_t* src, int32_t* dst,
                             int32_t* missing, const TableWs& ws, hipStream_t stream, LaunchHook hook) {
+  if (td.batch <= kTableThreads && td.batch * td.table_blocks + td.num_pages <= kOneWorkgroup)
+    return with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
+      hipLaunchKernelGGL(fork_kernel, dim3(1), dim3(kTableThreads), 0, stream, td, table, refs, seq_lens, parents,
+                         table_out, refs_out, seq_lens_out, src, dst, missing, ws.need, ws.map);
+    });
   hipError_t e = with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
     hipLaunchKernelGGL(fork_init_kernel, dim3((unsigned)((td.num_pages + 255) / 256)), dim3(256), 0, stream, td, refs,
                        refs_out);
@@ -752,11 +916,12 @@ hipError_t launch_page_fork(const eta_table_desc_t& td, const int32_t* table, co
 hipError_t launch_page_compact(const eta_table_desc_t& td, const int32_t* table, const int32_t* refs,
                                int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst,
                                int32_t* live, const TableWs& ws, hipStream_t stream, LaunchHook hook) {
+  const bool one = td.batch * td.table_blocks <= kOneWorkgroup;
   hipError_t e = with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
     hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(kTableThreads), 0, stream, td, refs, refs_out, src, dst, live,
-                       ws.map);
+                       ws.map, one ? table : nullptr, table_out);
   });
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || one) return e;
   return with_hook(hook, ETA_KERNEL_PAGE_TABLE, stream, [&] {
     hipLaunchKernelGGL(compact_table_kernel, dim3((unsigned)((td.table_blocks + 255) / 256), td.batch), dim3(256), 0,
                        stream, td, table, table_out, ws.map);

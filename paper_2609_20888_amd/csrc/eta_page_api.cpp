@@ -105,6 +105,40 @@ eta_status_t set_decode(int64_t n_blk_cap, Geom* g) {
   return ETA_OK;
 }
 
+// Splits per (sequence, kv head), each a workgroup; 0: the proportional plan.  One workgroup per
+// compute unit in all where a split of the longest sequence still has work for it; twice and four
+// times as many for batches, whose lengths differ, of half a million tokens and more (over the kv
+// heads).  us by workgroups in all, 128 dims: dense, 2 x 8000 tokens, 4 kv heads 128 / 256 / 512:
+// 11.9 / 10.8 / 13.6; 8 x 8000, 8 heads 256 / 512 / 1024: 26.6 / 24.7 / 28.7; 8 x 32K, 4 heads 39.7 /
+// 38.7 / 39.9; a step of 16 x 64K, 8 heads 512 / 1024 / 2048: 78 / 75 / 82, of 512K tokens 128 / 256:
+// 95 / 69.  A workgroup alone on a small share waits for its own loads (1000 tokens in one: 12.0, in
+// eight: 9.4).
+// The proportional plan deals workgroups by the lengths (or unions) that the kernel finds, at 2 to
+// 3 us: where equal shares would leave more than 64 units of 64 tokens (a step, which reads a part
+// of them: 128) of the longest sequence to one workgroup.
+// The smallest calls take one workgroup of eight wavefronts each, which writes its results itself:
+// a launch less, which the host takes 4 us for (dense, 2 x 1500 tokens of 64 dims: 10.4 us in a
+// graph against 8.9, but 11 against 13 launched one by one; a step of 4000: 13.8 against 14.9, and
+// 19 against 23).
+int page_plan(const Geom& g, bool dense) {
+  if (dense ? g.cap * g.D <= 1536 * 64 : g.cap * g.D * g.G <= 4096 * 64) return 1;
+  const int64_t BG = (int64_t)g.B * g.Hkv, units = (g.cap + 63) / 64, tokens = BG * g.cap;
+  const int64_t target = g.B == 1 || tokens < (int64_t(1) << 19) ? 256 : tokens < (int64_t(1) << 22) ? 512 : 1024;
+  int64_t S = (target + BG - 1) / BG;
+  const int64_t most = units / (dense ? 2 : 4);
+  if (S > most) S = most;
+  if (S > 256) S = 256;
+  if (S < 1) S = 1;
+  const bool dealt = BG <= kPropMaxGroups && (dense ? BG * (units + 2) < (int64_t(1) << 30) : BG * g.n_tiles <= kPropMaxCounts);
+  return g.B > 1 && dealt && units > S * (dense ? 64 : 128) ? 0 : (int)S;
+}
+
+SplitPlan page_splits(const Geom& g, int num_splits) {
+  const int S = num_splits > 0 ? num_splits : page_plan(g, false);
+  return S > 0 ? SplitPlan{S, S * g.B * g.Hkv} : plan_splits(g, 0);
+}
+int page_dense_splits(const Geom& g, int num_splits) { return num_splits > 0 ? num_splits : page_plan(g, true); }
+
 eta_status_t check_params(const eta_decode_params_t* p) {
   if (!p) return fail(ETA_ERR_INVALID_ARG, "params is NULL");
   if (!std::isfinite(p->beta) || p->beta < 0.f) return fail(ETA_ERR_INVALID_ARG, "beta must be finite and >= 0");
@@ -147,7 +181,7 @@ eta_status_t decode_impl(const eta_page_desc_t* pd, int32_t q_dtype, const void*
   if (eta_status_t st = check_index(summ, &pg.g)) return st;
   if (eta_status_t st = set_decode(summ->n_blk_cap, &pg.g)) return st;
   const Geom& g = pg.g;
-  const SplitPlan plan = plan_splits(g, p->num_splits);
+  const SplitPlan plan = page_splits(g, p->num_splits);
   DecodeWs ws;
   if (eta_status_t st = check_ws(workspace, workspace_bytes, decode_ws_bytes(g, plan, nullptr, nullptr))) return st;
   decode_ws_bytes(g, plan, &ws, workspace);
@@ -265,7 +299,7 @@ eta_status_t eta_page_decode_workspace_size(const eta_page_desc_t* pd, int64_t n
   if (eta_status_t st = set_decode(n_blk_cap, &pg.g)) return st;
   if (eta_status_t st = check_params(p)) return st;
   if (!bytes) return fail(ETA_ERR_INVALID_ARG, "bytes is NULL");
-  *bytes = decode_ws_bytes(pg.g, plan_splits(pg.g, p->num_splits), nullptr, nullptr);
+  *bytes = decode_ws_bytes(pg.g, page_splits(pg.g, p->num_splits), nullptr, nullptr);
   return ok();
 }
 
@@ -297,7 +331,7 @@ eta_status_t eta_page_dense_workspace_size(const eta_page_desc_t* pd, int32_t nu
   if (num_splits < 0 || num_splits > kMaxSplits)
     return fail(ETA_ERR_INVALID_ARG, "num_splits must be in [0, %d]", kMaxSplits);
   if (!bytes) return fail(ETA_ERR_INVALID_ARG, "bytes is NULL");
-  *bytes = dense_ws_bytes(pg.g, dense_splits(pg.g, num_splits), nullptr, nullptr);
+  *bytes = dense_ws_bytes(pg.g, page_dense_splits(pg.g, num_splits), nullptr, nullptr);
   return ok();
 }
 
@@ -316,7 +350,7 @@ eta_status_t eta_page_dense_decode(const eta_page_desc_t* pd, int32_t q_dtype, c
   if (!aligned16(q) || !aligned16(out) || !aligned4(table) || !aligned4(seq_lens))
     return fail(ETA_ERR_INVALID_ARG, "q and out must be 16-byte, table and seq_lens 4-byte aligned");
   const Geom& g = pg.g;
-  const int S = dense_splits(g, num_splits);
+  const int S = page_dense_splits(g, num_splits);
   DecodeWs ws;
   if (eta_status_t st = check_ws(workspace, workspace_bytes, dense_ws_bytes(g, S, nullptr, nullptr))) return st;
   dense_ws_bytes(g, S, &ws, workspace);

@@ -64,7 +64,6 @@ struct PageSplitArgs {
 
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kMaxGroup = 8;                 // query heads of a kv head
 constexpr int kItems = 256;                  // 64-token units resolved at a time
 constexpr uint32_t kIdMask = 0x00ffffffu;    // union id: block index | head bits << 24
@@ -100,6 +99,7 @@ __device__ __forceinline__ uint4 load16_nt(const uint8_t* p) {
 }
 
 // Exclusive prefix over the workgroup's threads; *total gets the sum.  Holds two barriers.
+template <int kWaves>
 __device__ __forceinline__ int block_excl_scan(int x, int* wsum, int* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int incl = wave_incl_scan(x);
@@ -289,8 +289,9 @@ __device__ __forceinline__ void store_o(void* o, int q_dtype, int64_t idx, float
     reinterpret_cast<__bf16*>(o)[idx] = (__bf16)x;
 }
 
-template <int D, int BS, bool DENSE, bool PROP, bool F32, int REP>
-__global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_kernel(PageSplitArgs a) {
+template <int D, int BS, bool DENSE, bool PROP, bool F32, int REP, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void page_split_kernel(PageSplitArgs a) {
+  constexpr int kThreads = 64 * kWaves;
   constexpr int GPT = kPropMaxGroups / kThreads, CPT = kPropMaxCounts / kThreads;
   const Geom& g = a.pg.g;
   const int G = g.G, tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_
   __shared__ int own_s[3];
   __shared__ int item_page[kItems];
   __shared__ uint32_t item_meta[kItems];           // head bits | sub << 8 | tokens << 16 | own token << 24
-  __shared__ float mrg_m[kWaves][16], mrg_l[kWaves][16];
+  __shared__ float mrg_m[kWaves][16], mrg_l[kWaves][16], sum_s[kMaxGroup];
   __shared__ __attribute__((aligned(16))) float mrg_acc[kWaves][16][D];
   __shared__ float rbest_s[DENSE ? 1 : kMaxGroup][kRescueTiles];
   __shared__ int rinfo_s[DENSE ? 1 : kMaxGroup][kRescueTiles];
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_
         cv[k] = run;
         run += x;
       }
-      const int ex = block_excl_scan(run, wsum_s, &tot);
+      const int ex = block_excl_scan<kWaves>(run, wsum_s, &tot);
 #pragma unroll
       for (int k = 0; k < CPT; ++k) pref_s[tid * CPT + k] = ex + cv[k];
       if (tid == 0) pref_s[kPropMaxCounts] = tot;
@@ -373,14 +374,14 @@ __global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_
       }
       mine += work[r];
     }
-    block_excl_scan(mine, wsum_s, &tot);
+    block_excl_scan<kWaves>(mine, wsum_s, &tot);
     int nsp[GPT], sum = 0, dummy;
 #pragma unroll
     for (int r = 0; r < GPT; ++r) {
       nsp[r] = tid * GPT + r < BG ? group_splits(work[r], tot, W, BG) : 0;
       sum += nsp[r];
     }
-    int f = block_excl_scan(sum, wsum_s, &dummy);
+    int f = block_excl_scan<kWaves>(sum, wsum_s, &dummy);
 #pragma unroll
     for (int r = 0; r < GPT; ++r) {
       if (tid * GPT + r < BG && owns_split(f, nsp[r], me)) {
@@ -443,7 +444,7 @@ __global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_
       for (int base = 0; base < g.n_tiles; base += kThreads) {
         const int t = base + tid;
         int tot;
-        const int ex = block_excl_scan(base == 0 ? tc0 : (t < g.n_tiles ? tc[t] : 0), wsum_s, &tot);
+        const int ex = block_excl_scan<kWaves>(base == 0 ? tc0 : (t < g.n_tiles ? tc[t] : 0), wsum_s, &tot);
         if (t < g.n_tiles) pref_s[t] = carry + ex;
         carry += tot;
       }
@@ -657,20 +658,25 @@ __global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) *reinterpret_cast<f32x4*>(&mrg_acc[w][col][16 * k + 4 * g4]) = st.acc[k];
   __syncthreads();
-  // wavefront 0, lane (w', column): the weight of that replica, the head's maximum and sum
-  float ms = kNegInf;
+  // wavefront 0, lane (w', column): the weights of the replicas of wavefronts w', w' + 4, ..; the
+  // heads' maxima and sums
   if (w == 0) {
-    const float mk = mrg_m[lane >> 4][col];
-    ms = mk;
-    for (int o = G; o < 16; o <<= 1) ms = fmaxf(ms, __shfl_xor(ms, o, 64));
-    ms = fmaxf(ms, __shfl_xor(ms, 16, 64));
-    ms = fmaxf(ms, __shfl_xor(ms, 32, 64));
-    const float wk = mk == kNegInf ? 0.f : __builtin_amdgcn_exp2f(mk - ms);
-    float L = mk == kNegInf ? 0.f : wk * mrg_l[lane >> 4][col];
+    float mk[kWaves / 4], ms = kNegInf, L = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves / 4; ++k) {
+      mk[k] = mrg_m[4 * k + g4][col];
+      ms = fmaxf(ms, mk[k]);
+    }
+    for (int o = G; o < 64; o <<= 1) ms = fmaxf(ms, __shfl_xor(ms, o, 64));
+#pragma unroll
+    for (int k = 0; k < kWaves / 4; ++k) {
+      const float wk = mk[k] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(mk[k] - ms);
+      if (mk[k] != kNegInf) L = fmaf(wk, mrg_l[4 * k + g4][col], L);
+      mrg_m[4 * k + g4][col] = wk;
+    }
     for (int o = G; o < 64; o <<= 1) L += __shfl_xor(L, o, 64);
-    mrg_m[lane >> 4][col] = wk;
     if (lane < G) {
-      mrg_l[0][lane] = L;
+      sum_s[lane] = L;
       if (!single) a.part_ml[(int64_t)(first + s) * G + lane] = make_float2(ms, L);
     }
   }
@@ -683,7 +689,7 @@ __global__ __launch_bounds__(kThreads, F32 && D == 128 ? 1 : 2) void page_split_
 #pragma unroll
       for (int j = 0; j < REP; ++j) o = fmaf(mrg_acc[k][j * G + h][i], mrg_m[k][j * G + h], o);
     if (single) {
-      const float L = mrg_l[0][h];
+      const float L = sum_s[h];
       store_o(a.out, a.q_dtype, (hq0 + h) * D + i, L == 0.f ? 0.f : o / L);
     } else {
       a.part_acc[((int64_t)(first + s) * G + h) * D + i] = o;
@@ -706,12 +712,17 @@ template <bool DENSE>
 void launch_split(const PageSplitArgs& a, const SplitPlan& pl, hipStream_t stream) {
   const Geom& g = a.pg.g;
   const dim3 grid = pl.S > 0 ? dim3(pl.S, g.Hkv, g.B) : dim3(pl.W);
-#define ETA_PSPL(D_, BS_, P_, F_)                                                                               \
-  if (g.D == D_ && g.BS == BS_ && (pl.S == 0) == P_ && (a.q_dtype == ETA_DT_F32) == F_) {                     \
-    if (g.G == 8)                                                                                             \
-      hipLaunchKernelGGL((page_split_kernel<D_, BS_, DENSE, P_, F_, 2>), grid, dim3(kThreads), 0, stream, a); \
-    else                                                                                                      \
-      hipLaunchKernelGGL((page_split_kernel<D_, BS_, DENSE, P_, F_, 4>), grid, dim3(kThreads), 0, stream, a); \
+#define ETA_PSPL_R(D_, BS_, P_, F_, R_, W_) \
+  hipLaunchKernelGGL((page_split_kernel<D_, BS_, DENSE, P_, F_, R_, W_>), grid, dim3(64 * W_), 0, stream, a);
+#define ETA_PSPL(D_, BS_, P_, F_)                                                          \
+  if (g.D == D_ && g.BS == BS_ && (pl.S == 0) == P_ && (a.q_dtype == ETA_DT_F32) == F_) {  \
+    if (g.G == 8) {                                                                        \
+      if (pl.S == 1) ETA_PSPL_R(D_, BS_, false, F_, 2, 8)                                  \
+      else ETA_PSPL_R(D_, BS_, P_, F_, 2, 4)                                               \
+    } else {                                                                               \
+      if (pl.S == 1) ETA_PSPL_R(D_, BS_, false, F_, 4, 8)                                  \
+      else ETA_PSPL_R(D_, BS_, P_, F_, 4, 4)                                               \
+    }                                                                                      \
   }
 #define ETA_PSPL_P(D_, BS_)                                           \
   ETA_PSPL(D_, BS_, false, false) ETA_PSPL(D_, BS_, false, true)      \
@@ -719,6 +730,7 @@ void launch_split(const PageSplitArgs& a, const SplitPlan& pl, hipStream_t strea
   ETA_PSPL_P(64, 64) ETA_PSPL_P(64, 128) ETA_PSPL_P(128, 64) ETA_PSPL_P(128, 128)
 #undef ETA_PSPL_P
 #undef ETA_PSPL
+#undef ETA_PSPL_R
 }
 
 }  // namespace

@@ -1269,8 +1269,7 @@ def fork_pages(table: torch.Tensor, refs: torch.Tensor, seq_lens: torch.Tensor, 
          ("src", o and o.src, None), ("dst", o and o.dst, None), ("missing", o and o.missing, 1)), (workspace,))
     if o is None:
         B = table.shape[0]
-        o = PageFork(_like_table(stream, table), _empty_like(stream, refs),
-                     *(_empty(stream, dev, torch.int32, m) for m in (B, B, B, 1)))
+        o, workspace = _table_results(PageFork, stream, dev, table, refs, (B, B, B, 1), workspace, nbytes)
     workspace = _workspace(workspace, nbytes, dev, stream)
     _launch(load_library().eta_page_fork, dev, stream, ref, table.data_ptr(), refs.data_ptr(), seq_lens.data_ptr(),
             parents.data_ptr(), o.table.data_ptr(), o.refs.data_ptr(), o.seq_lens.data_ptr(), o.src.data_ptr(),
@@ -1289,13 +1288,22 @@ def compact_pages(table: torch.Tensor, refs: torch.Tensor, *, out: Optional[Page
                                       (("src", o and o.src, half), ("dst", o and o.dst, half),
                                        ("live", o and o.live, 1)), (workspace,))
     if o is None:
-        o = PageCompaction(_like_table(stream, table), _empty_like(stream, refs),
-                           *(_empty(stream, dev, torch.int32, m) for m in (half, half, 1)))
+        o, workspace = _table_results(PageCompaction, stream, dev, table, refs, (half, half, 1), workspace, nbytes)
     workspace = _workspace(workspace, nbytes, dev, stream)
     _launch(load_library().eta_page_compact, dev, stream, ref, table.data_ptr(), refs.data_ptr(), o.table.data_ptr(),
             o.refs.data_ptr(), o.src.data_ptr(), o.dst.data_ptr(), o.live.data_ptr(), workspace.data_ptr(),
             workspace.numel() * workspace.element_size())
     return o
+
+
+def _table_results(kind, stream, dev, table, refs, sizes, workspace, nbytes):
+    """New results of a page-table call, the vectors of the given sizes as parts of one tensor, and
+    the workspace, which is another part of it unless one is given (4 us less on the host than
+    tensors of their own)."""
+    words = 0 if workspace is not None else (nbytes + 3) // 4
+    parts = _empty(stream, dev, torch.int32, words + sum(sizes)).split_with_sizes((words, *sizes))
+    return (kind(_like_table(stream, table), _empty_like(stream, refs), *parts[1:]),
+            parts[0] if workspace is None else workspace)
 
 
 def _like_table(stream, table: torch.Tensor) -> torch.Tensor:
