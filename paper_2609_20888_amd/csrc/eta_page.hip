@@ -70,11 +70,11 @@ __device__ __forceinline__ uint32_t scaled4(uint32_t w, float r) {
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   if constexpr (sizeof(T) == 4) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    const float4 a = __builtin_bit_cast(float4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p))), b = __builtin_bit_cast(float4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p) + 1));
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
     x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   } else {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint4 a = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs 
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = coded(x[r][e], inv);
-        *p = make_uint2(pack4(y[0], y[1], y[2], y[3]), pack4(y[4], y[5], y[6], y[7]));
+        __builtin_nontemporal_store((uint64_t)pack4(y[0], y[1], y[2], y[3]) | (uint64_t)pack4(y[4], y[5], y[6], y[7]) << 32, reinterpret_cast<uint64_t*>(p));
       } else if (t < lo && round_held) {
         const uint2 w = *p;
         *p = make_uint2(scaled4(w.x, again), scaled4(w.y, again));
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs 
   for (int k = tid; k < D * WPR; k += NT) {
     const int d = k / WPR, p = k % WPR;
     const uint32_t* s = &v_s[d][4 * p];
-    *reinterpret_cast<uint4*>(dst + d * BS + 16 * p) = make_uint4(s[0], s[1], s[2], s[3]);
+    __builtin_nontemporal_store(u32x4_t{s[0], s[1], s[2], s[3]}, reinterpret_cast<u32x4_t*>(dst + d * BS + 16 * p));
   }
 }
 
@@ -462,21 +462,27 @@ __global__ __launch_bounds__(256, 2) void page_summaries_kernel(IndexArgs a) {
 
 // ---------------------------------------------------------------- copies
 
-// One workgroup for a pair, a head, and K or V: b d codes and their scale.
+// One workgroup for a pair, a head, and K or V: b d codes (N x 256 x 16) and their scale.  Past
+// the caches when read (a copied page is not read next; 1200 pages of 256 KB: 37 us through them, 30
+// past them; written past them too: 33).
+template <int N>
 __global__ __launch_bounds__(256) void page_copy_kernel(eta_page_pool_t pool, PageGeom pg, const int32_t* src,
                                                         const int32_t* dst, int64_t n) {
   const int h = blockIdx.y >> 1;
   const bool isv = blockIdx.y & 1;
-  const int64_t bytes = (int64_t)pg.g.BS * pg.g.D;
-  uint8_t* code = reinterpret_cast<uint8_t*>(isv ? pool.v : pool.k);
-  float* scale = isv ? pool.v_scale : pool.k_scale;
+  uint8_t* code = reinterpret_cast<uint8_t*>(isv ? pool.v : pool.k) + (int64_t)h * (N * 4096) + threadIdx.x * 16;
+  float* scale = (isv ? pool.v_scale : pool.k_scale) + h;
   for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
     const int64_t a = src[i], b = dst[i];
     if (a < 0 || a >= pg.pages || b < 0 || b >= pg.pages) continue;
-    const uint4* from = reinterpret_cast<const uint4*>(code + a * pg.page_stride + h * bytes);
-    uint4* to = reinterpret_cast<uint4*>(code + b * pg.page_stride + h * bytes);
-    for (int k = threadIdx.x; k < bytes / 16; k += 256) to[k] = from[k];
-    if (threadIdx.x == 0) scale[b * pg.scale_stride + h] = scale[a * pg.scale_stride + h];
+    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(code + a * pg.page_stride);
+    u32x4_t* to = reinterpret_cast<u32x4_t*>(code + b * pg.page_stride);
+    u32x4_t x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = __builtin_nontemporal_load(from + 256 * k);
+#pragma unroll
+    for (int k = 0; k < N; ++k) to[256 * k] = x[k];
+    if (threadIdx.x == 0) scale[b * pg.scale_stride] = scale[a * pg.scale_stride];
   }
 }
 
@@ -871,7 +877,10 @@ hipError_t launch_page_copy(const PageGeom& pg, const eta_page_pool_t& pool, con
   if (n <= 0) return hipSuccess;
   const dim3 grid((unsigned)(n < 65536 ? n : 65536), 2 * pg.g.Hkv);
   return with_hook(hook, ETA_KERNEL_PAGE_COPY, stream, [&] {
-    hipLaunchKernelGGL(page_copy_kernel, grid, dim3(256), 0, stream, pool, pg, src, dst, n);
+    const int kb = pg.g.BS * pg.g.D / 4096;            // 4 KB pieces: 1, 2 or 4
+    if (kb == 1) hipLaunchKernelGGL(page_copy_kernel<1>, grid, dim3(256), 0, stream, pool, pg, src, dst, n);
+    if (kb == 2) hipLaunchKernelGGL(page_copy_kernel<2>, grid, dim3(256), 0, stream, pool, pg, src, dst, n);
+    if (kb == 4) hipLaunchKernelGGL(page_copy_kernel<4>, grid, dim3(256), 0, stream, pool, pg, src, dst, n);
   });
 }
 
