@@ -97,8 +97,16 @@ eta_status_t check_index(const eta_summary_t* s, Geom* g) {
   return set_index(s->n_blk_cap, g);
 }
 
+// Workgroups and partials are counted in 32 bits: at most 1024 splits of 2^20 groups.
+eta_status_t check_groups(const Geom& g) {
+  if ((int64_t)g.B * g.Hkv > (int64_t(1) << 20))
+    return fail(ETA_ERR_UNSUPPORTED, "batch * num_kv_heads must not exceed 2^20");
+  return ETA_OK;
+}
+
 // The decode's geometry: no sequence holds more full blocks than the index.
 eta_status_t set_decode(int64_t n_blk_cap, Geom* g) {
+  if (eta_status_t st = check_groups(*g)) return st;
   if (eta_status_t st = set_index(n_blk_cap, g)) return st;
   const int64_t most = n_blk_cap * g->BS + g->BS - 1;
   if (g->cap > most) g->cap = most;
@@ -328,6 +336,7 @@ eta_status_t eta_page_decode_predicted(const eta_page_desc_t* pd, int32_t q_dtyp
 eta_status_t eta_page_dense_workspace_size(const eta_page_desc_t* pd, int32_t num_splits, size_t* bytes) {
   PageGeom pg;
   if (eta_status_t st = check_pages(pd, true, &pg)) return st;
+  if (eta_status_t st = check_groups(pg.g)) return st;
   if (num_splits < 0 || num_splits > kMaxSplits)
     return fail(ETA_ERR_INVALID_ARG, "num_splits must be in [0, %d]", kMaxSplits);
   if (!bytes) return fail(ETA_ERR_INVALID_ARG, "bytes is NULL");
@@ -342,6 +351,7 @@ eta_status_t eta_page_dense_decode(const eta_page_desc_t* pd, int32_t q_dtype, c
   PageGeom pg;
   if (eta_status_t st = check_pages(pd, true, &pg)) return st;
   if (eta_status_t st = check_pool(pool)) return st;
+  if (eta_status_t st = check_groups(pg.g)) return st;
   if (!valid_dtype(q_dtype)) return fail(ETA_ERR_INVALID_ARG, "q_dtype %d is not ETA_DT_F32 or ETA_DT_BF16", q_dtype);
   if (num_splits < 0 || num_splits > kMaxSplits)
     return fail(ETA_ERR_INVALID_ARG, "num_splits must be in [0, %d]", kMaxSplits);
