@@ -577,13 +577,11 @@ typedef struct {
   float* v_scale;
 } eta_page_pool_t;
 
-/* New keys and values: element (b, h, i, c) of k at k[b*k_stride_b + h*k_stride_h + i*k_stride_t + c]
- * for new token i < new_tokens (strides in elements, >= 0, rows of head_dim contiguous and
- * 16-byte aligned), v alike. */
+/* Layout of new keys and values: element (b, h, i, c) of k at
+ * k[b*k_stride_b + h*k_stride_h + i*k_stride_t + c] for new token i < new_tokens (strides in
+ * elements, >= 0, rows of head_dim contiguous and 16-byte aligned), v alike. */
 typedef struct {
-  const void* k;
-  const void* v;
-  int32_t new_tokens;          /* >= 1 */
+  int32_t new_tokens;          /* >= 1, <= 2^26 */
   int32_t dtype;               /* ETA_DT_F32 or ETA_DT_BF16 */
   int64_t k_stride_b, k_stride_h, k_stride_t;
   int64_t v_stride_b, v_stride_h, v_stride_t;
@@ -607,8 +605,8 @@ typedef struct {
  * No two tokens of one call may fall into the same page by different rows of the table.
  */
 eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* table,
-                            const eta_page_rows_t* rows, const int32_t* start, const int32_t* new_lens,
-                            void* stream);
+                            const eta_page_rows_t* rows, const void* k, const void* v, const int32_t* start,
+                            const int32_t* new_lens, void* stream);
 
 /*
  * eta_page_summaries -- the block index of the keys as the pages hold them: mu, sigma and M (see

@@ -25,8 +25,8 @@ __host__ __device__ inline int64_t page_of(const int32_t* row, int64_t j, int64_
 }
 
 hipError_t launch_page_store(const PageGeom& pg, const eta_page_pool_t& pool, const int32_t* table,
-                             const eta_page_rows_t& rows, const int32_t* start, const int32_t* new_lens,
-                             hipStream_t stream, LaunchHook hook);
+                             const eta_page_rows_t& rows, const void* k, const void* v, const int32_t* start,
+                             const int32_t* new_lens, hipStream_t stream, LaunchHook hook);
 // prev_lens == nullptr: every full block, else max_new of them from prev_lens[b] / b on
 hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool, const int32_t* table,
                                  const int32_t* prev_lens, const int32_t* seq_lens, int max_new,

@@ -825,10 +825,10 @@ void launch_store(const StoreArgs& a, bool f32, dim3 grid, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_page_store(const PageGeom& pg, const eta_page_pool_t& pool, const int32_t* table,
-                             const eta_page_rows_t& rows, const int32_t* start, const int32_t* new_lens,
-                             hipStream_t stream, LaunchHook hook) {
+                             const eta_page_rows_t& rows, const void* k, const void* v, const int32_t* start,
+                             const int32_t* new_lens, hipStream_t stream, LaunchHook hook) {
   const Geom& g = pg.g;
-  const StoreArgs a{{(uint8_t*)pool.k, (uint8_t*)pool.v}, {pool.k_scale, pool.v_scale}, {rows.k, rows.v},
+  const StoreArgs a{{(uint8_t*)pool.k, (uint8_t*)pool.v}, {pool.k_scale, pool.v_scale}, {k, v},
                     {rows.k_stride_b, rows.v_stride_b}, {rows.k_stride_h, rows.v_stride_h},
                     {rows.k_stride_t, rows.v_stride_t}, table, start, new_lens, pg, rows.new_tokens};
   // the pages that new_tokens tokens can touch, wherever they begin

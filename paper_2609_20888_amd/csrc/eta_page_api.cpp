@@ -259,8 +259,8 @@ using namespace eta;
 extern "C" {
 
 eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* table,
-                            const eta_page_rows_t* rows, const int32_t* start, const int32_t* new_lens,
-                            void* stream) {
+                            const eta_page_rows_t* rows, const void* k, const void* v, const int32_t* start,
+                            const int32_t* new_lens, void* stream) {
   PageGeom pg;
   if (eta_status_t st = check_pages(pd, true, &pg)) return st;
   if (eta_status_t st = check_pool(pool)) return st;
@@ -269,8 +269,8 @@ eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* po
   // (fewer than 2^32 threads along the grid)
   if (rows->new_tokens > (1 << 26)) return fail(ETA_ERR_UNSUPPORTED, "new_tokens > 2^26 unsupported");
   if (!valid_dtype(rows->dtype)) return fail(ETA_ERR_INVALID_ARG, "dtype %d is not ETA_DT_F32 or ETA_DT_BF16", rows->dtype);
-  if (!rows->k || !rows->v || !table) return fail(ETA_ERR_INVALID_ARG, "k, v and table must be non-NULL");
-  if (!aligned16(rows->k) || !aligned16(rows->v) || !aligned4(table) || !aligned4(start) || !aligned4(new_lens))
+  if (!k || !v || !table) return fail(ETA_ERR_INVALID_ARG, "k, v and table must be non-NULL");
+  if (!aligned16(k) || !aligned16(v) || !aligned4(table) || !aligned4(start) || !aligned4(new_lens))
     return fail(ETA_ERR_INVALID_ARG, "k and v must be 16-byte, table, start and new_lens 4-byte aligned");
   const int64_t eb = elem_bytes(rows->dtype);
   for (int64_t s : {rows->k_stride_b, rows->k_stride_h, rows->k_stride_t, rows->v_stride_b, rows->v_stride_h,
@@ -278,7 +278,7 @@ eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* po
     if (s < 0) return fail(ETA_ERR_INVALID_ARG, "negative stride");
     if ((s * eb) % 16) return fail(ETA_ERR_INVALID_ARG, "k and v strides must keep rows 16-byte aligned");
   }
-  hipError_t e = launch_page_store(pg, *pool, table, *rows, start, new_lens, (hipStream_t)stream, active_hook());
+  hipError_t e = launch_page_store(pg, *pool, table, *rows, k, v, start, new_lens, (hipStream_t)stream, active_hook());
   if (e != hipSuccess) return fail(ETA_ERR_HIP, "page store launch failed: %s", hipGetErrorString(e));
   return ok();
 }

@@ -85,7 +85,7 @@ class PagePoolDesc(ctypes.Structure):
 
 
 class PageRows(ctypes.Structure):
-    _fields_ = [("k", _vp), ("v", _vp), ("new_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32)] + \
+    _fields_ = [("new_tokens", ctypes.c_int32), ("dtype", ctypes.c_int32)] + \
                [(n, ctypes.c_int64) for n in ("k_stride_b", "k_stride_h", "k_stride_t",
                                               "v_stride_b", "v_stride_h", "v_stride_t")]
 
@@ -166,7 +166,7 @@ def load_library(path: Optional[str] = None):
         "eta_qk_norm_rope": [P(RopeDesc)] + [_vp] * 12,
         "eta_qk_norm_rope_backward_workspace_size": [P(RopeDesc), P(sz)],
         "eta_qk_norm_rope_backward": [P(RopeDesc)] + [_vp] * 16 + [sz, _vp],
-        "eta_page_store": [P(PageDesc), P(PagePoolDesc), _vp, P(PageRows), _vp, _vp, _vp],
+        "eta_page_store": [P(PageDesc), P(PagePoolDesc), _vp, P(PageRows), _vp, _vp, _vp, _vp, _vp],
         "eta_page_summaries": [P(PageDesc), P(PagePoolDesc), _vp, _vp, _vp, i32, P(SummaryDesc), _vp],
         "eta_page_decode_workspace_size": [P(PageDesc), i64, P(DecodeParams), P(sz)],
         "eta_page_decode": [P(PageDesc), i32, _vp, P(PagePoolDesc), _vp, _vp, P(SummaryDesc), _vp,
@@ -968,8 +968,7 @@ class PagePool:
         return PagePool(codes(page, d), codes(d, page), *scales)
 
     def _desc(self) -> PagePoolDesc:
-        return PagePoolDesc(k=self.k.data_ptr(), v=self.v.data_ptr(), k_scale=self.k_scale.data_ptr(),
-                            v_scale=self.v_scale.data_ptr())
+        return PagePoolDesc(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
 
     def _form(self):
         return _form(self.k), _form(self.v), _form(self.k_scale), _form(self.v_scale)
@@ -1029,6 +1028,14 @@ def _query(q: torch.Tensor, pool: PagePool, table: torch.Tensor):
         raise ValueError(f"q must be [{table.shape[0]}][Hq][{pool.k.shape[3]}] contiguous, got {tuple(q.shape)}")
 
 
+_RECORDS = {torch.float32: ETA_DT_F32, torch.float16: ETA_DT_F16, E4M3: ETA_DT_FP8}
+
+
+def _index_desc(s: Summaries) -> SummaryDesc:
+    """Summaries.desc by position (half a microsecond less)."""
+    return SummaryDesc(s.mu.data_ptr(), s.sigma.data_ptr(), s.max_norm.data_ptr(), s.mu.shape[-1], _RECORDS[s.mu.dtype], 0)
+
+
 def _summ_form(s: Summaries):
     return _form(s.mu), _form(s.sigma), _form(s.max_norm)
 
@@ -1053,11 +1060,11 @@ def store_pages(k: torch.Tensor, v: torch.Tensor, pool: PagePool, table: torch.T
         _vector("start", start, B, torch.int32)
         _vector("new_lens", new_lens, B, torch.int32)
         steps = {f"{n}_stride_{x}": _step(t, i) for n, t in (("k", k), ("v", v)) for i, x in enumerate("bht")}
-        return pd, ctypes.byref(pd), dev, dict(new_tokens=k.shape[2], dtype=dt, **steps)
+        rows = PageRows(new_tokens=k.shape[2], dtype=dt, **steps)
+        return (pd, rows), ctypes.byref(pd), dev, ctypes.byref(rows)
     _, ref, dev, rows = _plan((3, _form(k), _form(v), pool._form(), _form(table), _form(start), _form(new_lens)), make)
-    r = PageRows(k=k.data_ptr(), v=v.data_ptr(), **rows)
-    _launch(load_library().eta_page_store, dev, stream, ref, ctypes.byref(pool._desc()), table.data_ptr(),
-            ctypes.byref(r), _at(start), _at(new_lens))
+    _launch(load_library().eta_page_store, dev, stream, ref, ctypes.byref(pool._desc()), table.data_ptr(), rows,
+            k.data_ptr(), v.data_ptr(), _at(start), _at(new_lens))
     return pool
 
 
@@ -1093,7 +1100,7 @@ def _page_summaries(pool, table, prev_lens, seq_lens, max_new, summ, stream):
         return pd, ctypes.byref(pd), dev
     _, ref, dev = _plan((4, pool._form(), _form(table), _form(prev_lens), _form(seq_lens), _summ_form(summ)), make)
     _launch(load_library().eta_page_summaries, dev, stream, ref, ctypes.byref(pool._desc()), table.data_ptr(),
-            _at(prev_lens), seq_lens.data_ptr(), int(max_new), ctypes.byref(summ.desc()))
+            _at(prev_lens), seq_lens.data_ptr(), int(max_new), ctypes.byref(_index_desc(summ)))
     return summ
 
 
@@ -1130,7 +1137,7 @@ def _decode_pages(q, pool, table, seq_lens, summ, tau, W, bias, params, out, mas
                                                       stream)
     workspace = _workspace(workspace, nbytes, dev, stream)
     lib, common = load_library(), (dt, q.data_ptr(), ctypes.byref(pool._desc()), table.data_ptr(), seq_lens.data_ptr(),
-                                   ctypes.byref(summ.desc()))
+                                   ctypes.byref(_index_desc(summ)))
     results = (ctypes.byref(p), out.data_ptr(), mask.data_ptr(), _at(counts), _at(union_counts))
     space = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     if bias is None:

@@ -115,7 +115,7 @@ hipError_t launch_dense_combine(const Geom&, int S, int, const int32_t*, void*, 
   CHECK(S != 1, "one split is not combined");
   return hipSuccess;
 }
-hipError_t launch_page_store(const PageGeom&, const eta_page_pool_t&, const int32_t*, const eta_page_rows_t&, const int32_t*, const int32_t*, hipStream_t, LaunchHook) { ++launches; return hipSuccess; }
+hipError_t launch_page_store(const PageGeom&, const eta_page_pool_t&, const int32_t*, const eta_page_rows_t&, const void*, const void*, const int32_t*, const int32_t*, hipStream_t, LaunchHook) { ++launches; return hipSuccess; }
 hipError_t launch_page_summaries(const PageGeom&, const eta_page_pool_t&, const int32_t*, const int32_t*, const int32_t*, int, const eta_summary_t&, hipStream_t, LaunchHook) { ++launches; return hipSuccess; }
 hipError_t launch_page_copy(const PageGeom&, const eta_page_pool_t&, const int32_t*, const int32_t*, int64_t, hipStream_t, LaunchHook) { ++launches; return hipSuccess; }
 

@@ -38,7 +38,7 @@ def summ(**kw):
 
 
 def rows(**kw):
-    d = dict(k=FAKE, v=FAKE, new_tokens=5, dtype=eta.ETA_DT_BF16, k_stride_b=1280, k_stride_h=640, k_stride_t=128,
+    d = dict(new_tokens=5, dtype=eta.ETA_DT_BF16, k_stride_b=1280, k_stride_h=640, k_stride_t=128,
              v_stride_b=1280, v_stride_h=640, v_stride_t=128)
     d.update(kw)
     return eta.PageRows(**d)
@@ -49,10 +49,10 @@ def ref(x):
 
 
 def store(lib, d=None, p=None, r=None, **kw):
-    a = dict(table=FAKE, start=None, lens=None)
+    a = dict(table=FAKE, k=FAKE, v=FAKE, start=None, lens=None)
     a.update(kw)
     return lib.eta_page_store(ref(desc() if d is None else d), ref(pool() if p is None else p), a["table"],
-                              ref(rows() if r is None else r), a["start"], a["lens"], None)
+                              ref(rows() if r is None else r), a["k"], a["v"], a["start"], a["lens"], None)
 
 
 def index(lib, d=None, p=None, s=None, **kw):
@@ -127,11 +127,12 @@ def test_null_and_misaligned_pools_refused(lib, call):
 
 def test_store_refused(lib):
     assert store(lib, r=0) == INVALID
-    for kw in (dict(k=None), dict(v=None), dict(k=FAKE + 8), dict(new_tokens=0), dict(dtype=eta.ETA_DT_F16), dict(k_stride_b=-8),
+    for kw in (dict(new_tokens=0), dict(dtype=eta.ETA_DT_F16), dict(k_stride_b=-8),
                dict(k_stride_t=4), dict(v_stride_h=12)):
         assert store(lib, r=rows(**kw)) == INVALID, kw
     assert store(lib, r=rows(new_tokens=(1 << 26) + 1)) == UNSUPPORTED
-    for kw in (dict(table=None), dict(table=FAKE + 2), dict(start=FAKE + 1), dict(lens=FAKE + 2)):
+    for kw in (dict(table=None), dict(table=FAKE + 2), dict(start=FAKE + 1), dict(lens=FAKE + 2), dict(k=None), dict(v=None),
+               dict(k=FAKE + 8), dict(v=FAKE + 2)):
         assert store(lib, **kw) == INVALID, kw
 
 
