@@ -43,7 +43,7 @@ hipError_t launch_page_dense(const PageGeom& pg, const SplitPlan& plan, int q_dt
                              const eta_page_pool_t& pool, const int32_t* table, const int32_t* seq_lens,
                              void* out, const DecodeWs& ws, hipStream_t stream, LaunchHook hook);
 
-// Page tables.  ws: kTableWsInts(td) 32-bit words.
+// Page tables.
 struct TableWs {
   int32_t* need;     // [batch] pages that each row asks for
   int32_t* map;      // [num_pages] a page's new number, or the free pages in order

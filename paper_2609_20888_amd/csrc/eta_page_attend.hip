@@ -10,16 +10,27 @@
 // 16 columns, four tiles of 16 keys.  Row i of tile t is token 16 (i / 4) + 4 t + i % 4, so that
 // the result hands lane (column, lane group g) the tokens 16 g + 4 t + r.  The columns repeat the
 // group's heads (column G j + h: head h), and replica j takes the gate and the softmax of its
-// share of the tiles alone, so that every lane has scores of its own to work on (one replica and
-// idle columns: four heads, 512K tokens, 71 -> us).  The weights are, as they lie, the B operand
-// of p.V, with zeros for the other replicas' tokens: A = 16 dims x 32 tokens of V, which lies by
-// dimension in the page, so that lane (dim, g) reads its 16 tokens with one 16-byte load.  The
-// result is the output's transpose, columns as before: the softmax state and the rescaling stay
-// in the lane, each replica has its own, and they are merged once at the end.  The contraction
-// runs in the order the loads give (any order does that both operands share).
+// share of the tiles alone, so that a lane has 4 scores (eight heads: 8) to work on, not 16 in a
+// quarter of the lanes.  The weights are, as they lie, the B operand of p.V, with zeros for the
+// other replicas' tokens: A = 16 dims x 32 tokens of V, which lies by dimension in the page, so
+// that lane (dim, g) reads its 16 tokens with one 16-byte load.  The result is the output's
+// transpose, columns as before: the softmax state and the rescaling stay in the lane, each replica
+// has its own, and they are merged once at the end.  The contraction runs in the order the loads
+// give (any order does that both operands share).
 //
 // The weights go to p.V as two bf16 parts (16 bits), and fp32 queries as three with weights of
-// three: MFMA time is not what bounds these kernels.
+// three: the time of the matrix cores does not bound these kernels.  One part would add 2^-9 of
+// each weight, as much as the bf16 output's own rounding; fp16 would lose weights below 2^-24,
+// which a long context has many of beside one that stands out.
+//
+// Bound by HBM once the caches are long: without the gate, the softmax and p.V the same loads take
+// the same time.  512K tokens, 4 kv heads, d = 128, 283.7 MB of a step's union: 48.4 us (5.9 TB/s; a
+// device copy reads and writes 5.16); 8 ragged sequences of up to 32K, dense: 185 MB in 33.4 us;
+// 16 of up to 64K, 232.5 MB of unions in 48.9 us.  Of these 4 to 6 us are the way to the first
+// load (length, tile counts, union ids, page, keys: each needs the one before) and the merge; short
+// calls are nothing else.  Tried and not faster: values a unit further ahead in a second buffer,
+// eight wavefronts, three per SIMD, the merge by the last workgroup of a group instead of a launch
+// (69 -> 82 us a step: every workgroup's release writes its L2 back).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
