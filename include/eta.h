@@ -602,7 +602,8 @@ typedef struct {
  * and the same codes wherever no code fell below 2^-6 on the way.
  *   start, new_lens  device int32 [batch], or NULL: 0, new_tokens (start below 0 counts as 0,
  *                    new_lens are clamped to [0, new_tokens])
- * No two tokens of one call may fall into the same page by different rows of the table.
+ * No two tokens of one call may fall into the same page by two entries of the table (its contents
+ * would be undefined).
  */
 eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* table,
                             const eta_page_rows_t* rows, const void* k, const void* v, const int32_t* start,
@@ -612,7 +613,8 @@ eta_status_t eta_page_store(const eta_page_desc_t* pd, const eta_page_pool_t* po
  * eta_page_summaries -- the block index of the keys as the pages hold them: mu, sigma and M (see
  * eta_build_block_summaries; flat sigma) of every full block, or, with prev_lens, of blocks
  * prev_lens[b] / b .. + max_new_blocks - 1 that are full (see eta_update_block_summaries).
- * Blocks past n_blk_cap, and those without a page, are not written.
+ * Blocks past n_blk_cap, and those without a page, are not written.  A key with NaN makes its
+ * block's bound NaN, and with it mu and sigma of up to 32 dimensions.
  */
 eta_status_t eta_page_summaries(const eta_page_desc_t* pd, const eta_page_pool_t* pool, const int32_t* table,
                                 const int32_t* prev_lens, const int32_t* seq_lens, int32_t max_new_blocks,
@@ -689,7 +691,7 @@ eta_status_t eta_page_extend(const eta_table_desc_t* td, int32_t* table, int32_t
  *   table, refs, seq_lens         as they were;  table_out, refs_out, seq_lens_out: the new ones
  *   src, dst  int32 [batch]: for each row the page to copy and its own new one, or -1, -1
  *   missing   int32 [1]: how many rows found no free page (their last block's entry is -1)
- * No output may overlap an input or another output.
+ * No output may overlap an input or another output (a table: from its first row to its last).
  */
 eta_status_t eta_page_fork(const eta_table_desc_t* td, const int32_t* table, const int32_t* refs,
                            const int32_t* seq_lens, const int32_t* parents, int32_t* table_out,

@@ -287,7 +287,9 @@ __global__ __launch_bounds__(256) void page_token_kernel(StoreArgs a) {
 //           come back 5e-6 off, of bf16 ones 3e-8.)
 // The block stays in registers for both passes (two passes: mean first, so that a coordinate
 // whose mean is far larger than its spread loses nothing).  Results are staged in LDS and leave
-// as rows of the dimension-major records.
+// as rows of the dimension-major records.  (NaN times a zero of the unit matrix is NaN: a key with
+// NaN makes the means and deviations of the 32 dims beside it NaN too; the block's bound is NaN
+// with one of them.)
 
 struct IndexArgs {
   const uint8_t* k;

@@ -224,10 +224,11 @@ struct Attend {
       bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
       bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
       const bool first = st.t == kNegInf;
-      const float mn = first ? (bm == kNegInf ? 0.f : bm) : fmaxf(st.m, bm);
+      // (a reference is a number: where every score is NaN, the weights are)
+      const float mn = first ? (bm > kNegInf ? bm : 0.f) : fmaxf(st.m, bm);
       const float alpha = first ? 1.0f : __builtin_amdgcn_exp2f(st.m - mn);   // (before the first key: of zeros)
       st.m = mn;
-      if (!first || bm != kNegInf) st.t = mn + 8.0f;
+      if (!first || bm > kNegInf) st.t = mn + 8.0f;
       st.l *= alpha;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) st.acc[k] *= alpha;
@@ -459,10 +460,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_split_kernel(PageSplitArg
         if (t < g.n_tiles) pref_s[t] = carry + ex;
         carry += tot;
       }
-      if (tid == 0) {
-        pref_s[g.n_tiles] = carry;
-        if (s == 0) a.plan[bg] = make_int2(first, S);
-      }
+      if (tid == 0) pref_s[g.n_tiles] = carry;
       UI = carry;
     }
     __syncthreads();
@@ -604,7 +602,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_split_kernel(PageSplitArg
     const uint32_t meta = __builtin_amdgcn_readfirstlane(item_meta[x]);
     const float ks = ks_n, vs = vs_n;
     const int n = (meta >> 16) & 255;
-    const bool on = at.rep < REP && ((meta >> head) & 1u);
+    // (a unit without a page is not attended: what was read in its place weighs nothing, NaN or not)
+    const bool on = at.rep < REP && n > 0 && ((meta >> head) & 1u);
     constexpr int NS = Attend<D, DENSE, F32, REP>::NS;
     float c[NS], p[NS];
     if constexpr (more) next(x + kWaves);
@@ -663,7 +662,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_split_kernel(PageSplitArg
   st.l += __shfl_xor(st.l, 16, 64);
   st.l += __shfl_xor(st.l, 32, 64);
   if (g4 == 0) {
-    mrg_m[w][col] = st.t == kNegInf ? kNegInf : st.m;          // (idle columns: none)
+    // (no key: no weight; keys whose scores are all NaN leave t as it was, and a sum of NaN)
+    mrg_m[w][col] = st.t == kNegInf && st.l == 0.f ? kNegInf : st.m;
     mrg_l[w][col] = st.l;
   }
 #pragma unroll
@@ -688,7 +688,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_split_kernel(PageSplitArg
     for (int o = G; o < 64; o <<= 1) L += __shfl_xor(L, o, 64);
     if (lane < G) {
       sum_s[lane] = L;
-      if (!single) a.part_ml[(int64_t)(first + s) * G + lane] = make_float2(ms, L);
+      // (the merge takes a sum that is not positive for no key: NaN goes on in the accumulators)
+      if (!single) a.part_ml[(int64_t)(first + s) * G + lane] = make_float2(ms, L != L ? 1.0f : L);
     }
   }
   __syncthreads();
@@ -699,11 +700,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_split_kernel(PageSplitArg
     for (int k = 0; k < kWaves; ++k)
 #pragma unroll
       for (int j = 0; j < REP; ++j) o = fmaf(mrg_acc[k][j * G + h][i], mrg_m[k][j * G + h], o);
+    const float L = sum_s[h];
     if (single) {
-      const float L = sum_s[h];
       store_o(a.out, a.q_dtype, (hq0 + h) * D + i, L == 0.f ? 0.f : o / L);
     } else {
-      a.part_acc[((int64_t)(first + s) * G + h) * D + i] = o;
+      a.part_acc[((int64_t)(first + s) * G + h) * D + i] = L != L ? L : o;
     }
   }
   if constexpr (!DENSE) {

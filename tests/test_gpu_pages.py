@@ -314,6 +314,59 @@ def test_pages_missing_shared_and_apart():
                 ps.close(out[b, r].cpu(), want, tol, mass, BF)
 
 
+@pytest.mark.parametrize("splits", [0, 1, 5])
+def test_entries_without_a_page_beside_a_page_of_nan(splits):
+    """What is read in an absent page's place has no say, whatever it holds."""
+    c = Case(2, 2, 4, 64, 64, [64 * 10 + 20, 64 * 9], BF, share=0.6)
+    c.table[c.table == 0] = min(set(range(1, c.P)) - set(c.table.flatten().tolist()))     # page 0 is in no row
+    assert 0 not in c.table
+    c.refresh()
+    c.table[0, 3] = c.table[1, 2] = -1
+    for t in (c.pool.k.view(torch.uint8), c.pool.v.view(torch.uint8)):
+        t[0] = 0x7f
+    c.pool.k_scale[0] = c.pool.v_scale[0] = math.nan
+    c.check(c.run(num_splits=splits))
+    out = eta.dense_decode_pages(c.q.cuda(), c.pool, c.table.cuda(), ints(*c.lens), num_splits=splits)
+    assert not out.isnan().any()
+
+
+@pytest.mark.parametrize("splits", [0, 1, 5])
+@pytest.mark.parametrize("T", [64 * 12 + 9, 64 * 90])
+def test_nan_reaches_the_heads_that_attend_it(T, splits):
+    """NaN in a query, a threshold, an attended key or value: those outputs, and no others."""
+    def outs(c):
+        return (c.run(num_splits=splits).out, eta.dense_decode_pages(c.q.cuda(), c.pool, c.table.cuda(), ints(*c.lens), num_splits=splits))
+    c = Case(1, 2, 4, 128, 64, [T], BF)
+    want = outs(c)
+    mask = c.run(num_splits=splits).mask[0].cpu().bool()
+    c.q[0, 2, 7] = math.nan
+    step, dense = outs(c)
+    assert dense[0, 2].isnan().all() and (step[0, 2].isnan().all() if T % 64 else not step[0, 2].any())   # (a NaN bound selects nothing)
+    # A tile's heads are scaled down together, when any of them needs it, and share their union's blocks: heads beside
+    # the one of NaN are joined in another order of the same sums, each within the bounds of the plain form.
+    for r in (0, 1, 3, 4, 7):
+        k, there = c.host.rows(c.table, 0, r // 4, T, "k")
+        v, _ = c.host.rows(c.table, 0, r // 4, T, "v")
+        blocks = torch.cat([mask[r, :T // 64], torch.ones(1 if T % 64 else 0, dtype=torch.bool)])
+        q = c.q[0, r].double()
+        ps.close(step[0, r].cpu(), *ps.attend(q, k, v, there, blocks, 64, tau=c.tau[0, r].double(), beta=4.0), BF)
+        ps.close(dense[0, r].cpu(), *ps.attend(q, k, v, there, None, 64), BF)
+    for r in (4, 7):
+        assert torch.equal(dense[0, r], want[1][0, r])
+    c = Case(1, 2, 4, 128, 64, [T], BF)
+    j = int(torch.nonzero(mask[4:].any(0))[0])
+    c.pool.k.view(torch.uint8)[int(c.table[0, j]), 1, 5, 9] = 0x7f
+    step, dense = outs(c)
+    for r in range(8):
+        assert dense[0, r].isnan().all() == (r >= 4) and torch.equal(step[0, r].isnan(), (mask[r, j] & (r >= 4)).cuda().expand(128))
+    c = Case(1, 2, 4, 128, 64, [T], BF)
+    c.pool.v.view(torch.uint8)[int(c.table[0, j]), 1, 9, 5] = 0x7f
+    step, dense = outs(c)
+    for r in range(8):
+        assert dense[0, r].isnan().nonzero().flatten().tolist() == ([9] if r >= 4 else [])
+        assert step[0, r].isnan().nonzero().flatten().tolist() == ([9] if r >= 4 and mask[r, j] else [])
+
+
 @pytest.mark.parametrize("page", [64, 128])
 def test_nan_in_masked_places(page):
     """NaN behind a sequence's end and in blocks that a head does not attend reaches no result."""
