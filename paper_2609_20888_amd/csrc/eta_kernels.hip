@@ -732,6 +732,7 @@ struct ScreenArgs {
   int predict;
   float z, offset_a;
   int c, lwb, screen_all;
+  int by_length;
 };
 
 constexpr int kScreenThreads = 256;
@@ -801,10 +802,25 @@ __global__ __launch_bounds__(kScreenThreads) void screen_kernel(ScreenArgs a) {
     jm = jm < g.ncap ? jm : g.ncap - 1;
     M = a.mx[bg * g.ncap + jm];       // (used by wavefront 0)
   };
+  // A tile behind the sequence's full blocks selects nothing, and with `by_length` none of it is
+  // read: the index of a cache with room to spare costs what is in it.
+  const int64_t T = clamp_len(a.seq_lens, b, g.cap);
+  if constexpr (!BOUNDS_ONLY) {
+    if (a.by_length && tile > 0 && T < ((int64_t)tile * kScreenTile + 1) * g.BS) {
+      if (w != 0) return;
+      const int64_t j = (int64_t)tile * kScreenTile + lane;
+      if (j < g.ncap) {
+#pragma unroll
+        for (int h = 0; h < G; ++h) a.mask[(hq0 + h) * g.ncap + j] = 0;
+      }
+      if (lane == 0) a.tile_cnt[bg * g.n_tiles + tile] = 0;
+      if (lane < G) a.head_cnt[(hq0 + lane) * g.n_tiles + tile] = 0;
+      return;
+    }
+  }
   // the bias (or given threshold) and the predictor rows first, then this
   // tile's summaries: each is consumed in that order, so no wait for a later
   // load holds up an earlier step
-  const int64_t T = clamp_len(a.seq_lens, b, g.cap);
   float tau_in = 0.f;
   if (!BOUNDS_ONLY && tid < G) tau_in = a.predict ? a.bias[gh * G + tid] : a.tau[hq0 + tid];
   // this wavefront's query elements: heads w, w + 4, ..., dimensions lane + 64 s
@@ -2496,6 +2512,11 @@ void launch_combine_impl(const Geom& g, const CombineArgs& ca, hipStream_t strea
 
 // L2 bytes of W that the fused predictor may re-read per step (see launch_decode)
 constexpr int64_t kFusedPredictMaxBytes = 64ll << 20;
+// Screening workgroups (four a compute unit) that run at once.  Past them every workgroup looks at
+// its sequence's length first: the steps of 8 x 8000 tokens, 8 kv heads of 128 dims, with room for
+// 256K each took 63 us and take 35, full ones of 16 x 64K 75 both.  Fewer would only wait for it
+// (a step of 4000 tokens 0.1 us longer, of 4000 with room for 256K 1 us shorter).
+constexpr int64_t kScreenAtOnce = 1024;
 
 hipError_t launch_screen(const Geom& g, const DecodeCfg& c, int q_dtype, const void* q,
                          const int32_t* seq_lens, const eta_summary_t& s, const float* tau,
@@ -2516,7 +2537,8 @@ hipError_t launch_screen(const Geom& g, const DecodeCfg& c, int q_dtype, const v
   ScreenArgs sa{q, seq_lens, separate ? ws.tau : tau, W, bias, ws.tau, tau_out, s.mu, s.sigma,
                 s.max_norm, mask, ws.ids, ws.tile_cnt, ws.head_cnt, nullptr, ws.resc_best,
                 ws.resc_info, ws.wbits, g, q_dtype, (predict && !separate) ? 1 : 0, c.z,
-                c.offset_a, c.rescue_window, c.lwb, c.screen_all};
+                c.offset_a, c.rescue_window, c.lwb, c.screen_all,
+                (int64_t)g.B * g.Hkv * g.n_tiles > kScreenAtOnce};
   return with_hook(hook, ETA_KERNEL_SCREEN, stream,
                    [&] { launch_screen_impl<false>(g, sa, stream); });
 }

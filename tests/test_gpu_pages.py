@@ -260,6 +260,19 @@ def test_decode_short(lens):
         c.check(c.run())
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(lwb=70), dict(screen_all=True)])
+@pytest.mark.parametrize("page", [64, 128])
+def test_room_to_spare(page, kw):
+    """Lengths about the ends of the index's tiles of 64 blocks, in few tiles and in more than run at once, most of
+    which have no tokens."""
+    ends = [0, page - 1, 64 * page - 1, 64 * page, 65 * page - 1, 65 * page, 128 * page + 5, 129 * page]
+    c = Case(16, 2, 4, 64, page, ends + ends[::-1], BF)
+    c.check(c.run(**kw), **kw)
+    c.table = torch.cat([c.table, torch.full((16, 64 * 33 - c.table.shape[1]), -1, dtype=torch.int32)], 1)
+    c.refresh()
+    c.check(c.run(**kw), **kw)
+
+
 @pytest.mark.parametrize("kw", [dict(lwb=3), dict(rescue_window=0), dict(self_ungated=True), dict(offset_a=0.3),
                                 dict(screen_all=True), dict(num_splits=1), dict(num_splits=3), dict(num_splits=64)])
 def test_decode_parameters(kw):
