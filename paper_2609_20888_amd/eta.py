@@ -1043,10 +1043,10 @@ def _summ_form(s: Summaries):
 def store_pages(k: torch.Tensor, v: torch.Tensor, pool: PagePool, table: torch.Tensor, *,
                 start: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
                 stream=None) -> PagePool:
-    """eta_page_store: rounds new keys and values k, v [B][Hkv][T][d] (float32 or bfloat16, any
-    strides, the head dimension contiguous) into the pages that table int32 [B][blocks] lists:
-    token i of sequence b at position start[b] + i, for i < new_lens[b] (None: 0 and T).  Returns
-    the pool, changed in place."""
+    """eta_page_store: rounds new keys and values k, v [B][Hkv][T][d] (float32 or bfloat16, the
+    head dimension contiguous, any strides that keep rows 16-byte aligned) into the pages that
+    table int32 [B][blocks] lists: token i of sequence b at position start[b] + i, for
+    i < new_lens[b] (None: 0 and T).  Returns the pool, changed in place."""
     def make():
         dt = _dtype_code(k)
         dev = _on_one_gpu(k, v, pool.k, pool.v, pool.k_scale, pool.v_scale, table, start, new_lens)
