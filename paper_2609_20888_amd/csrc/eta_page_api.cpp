@@ -113,26 +113,32 @@ eta_status_t set_decode(int64_t n_blk_cap, Geom* g) {
   return ETA_OK;
 }
 
-// Splits per (sequence, kv head), each a workgroup; 0: the proportional plan.  One workgroup per
-// compute unit in all where a split of the longest sequence still has work for it; twice and four
-// times as many for batches, whose lengths differ, of half a million tokens and more (over the kv
-// heads).  us by workgroups in all, 128 dims: dense, 2 x 8000 tokens, 4 kv heads 128 / 256 / 512:
-// 11.9 / 10.8 / 13.6; 8 x 8000, 8 heads 256 / 512 / 1024: 26.6 / 24.7 / 28.7; 8 x 32K, 4 heads 39.7 /
-// 38.7 / 39.9; a step of 16 x 64K, 8 heads 512 / 1024 / 2048: 78 / 75 / 82, of 512K tokens 128 / 256:
-// 95 / 69.  A workgroup alone on a small share waits for its own loads (1000 tokens in one: 12.0, in
-// eight: 9.4).
+// Splits per (sequence, kv head), each a workgroup; 0: the proportional plan.  256 workgroups in all
+// (one a compute unit, of the two that fit at once), 512 for batches of a million tokens and more
+// over the kv heads, 1024, whose order evens out different lengths, past 2^22.  Not more than that (a
+// few left over take as long as a whole round: dense, 3 x 21K tokens, 8 kv heads 504 / 528: 26.8 / 37.5
+// us) unless an eighth of them would be missing: then 512 (100 groups of 6000 tokens 300 / 500: 29.5 /
+// 27.7), or one more split (192 groups of 16K tokens 384 / 576: 83 / 74).  us by workgroups in all, 128 dims: dense, 2 x 8000 tokens, 4 kv heads 128 / 256 / 512:
+// 11.8 / 10.7 / 13.6; 8 x 8000, 8 heads 32.4 / 24.4 / 24.9; 8 x 32K, 4 heads 256 / 512 / 1024 39.1 /
+// 38.2 / 38.7; a step of 2 x 158K, 2 heads 22.9 / 26.1 / 37.9, 16 x 16K, 8 heads 57.3 / 55.4 / 55.7, 16 x
+// 64K 166 / 161 / 152, of 512K tokens 128 / 256: 95 / 69.  A workgroup alone on a small share waits for
+// its own loads (1000 tokens in one: 12.0, in eight: 9.4).
 // The proportional plan deals workgroups by the lengths (or unions) that the kernel finds, at 2 to
 // 3 us: where equal shares would leave more than 64 units of 64 tokens (a step, which reads a part
 // of them: 128) of the longest sequence to one workgroup.
-// The smallest calls take one workgroup of eight wavefronts each, which writes its results itself:
-// a launch less, which the host takes 4 us for (dense, 2 x 1500 tokens of 64 dims: 10.4 us in a
-// graph against 8.9, but 11 against 13 launched one by one; a step of 4000: 13.8 against 14.9, and
-// 19 against 23).
+// One workgroup of eight wavefronts for each writes the results itself, a launch less: where the
+// groups alone fill the card and are not long (a step of 32 x 4000, 8 heads: 33.0 / in two 37.8; dense
+// 35.4 / 40.9; 24 x 4000 31.9 / 35.6; equal at 16K), and for the smallest calls, whose launches the
+// host takes 4 us for (dense, 2 x 1500 tokens of 64 dims: 10.4 us in a graph against 8.9, but 11
+// against 13 launched one by one; a step of 4000: 13.6 against 14.5, and 20 against 23).
 int page_plan(const Geom& g, bool dense) {
-  if (dense ? g.cap * g.D <= 1536 * 64 : g.cap * g.D * g.G <= 4096 * 64) return 1;
+  if (dense ? g.cap * g.D <= 1536 * 64 : g.cap * g.D * g.G <= 6000 * 64) return 1;
   const int64_t BG = (int64_t)g.B * g.Hkv, units = (g.cap + 63) / 64, tokens = BG * g.cap;
-  const int64_t target = g.B == 1 || tokens < (int64_t(1) << 19) ? 256 : tokens < (int64_t(1) << 22) ? 512 : 1024;
-  int64_t S = (target + BG - 1) / BG;
+  if (BG >= 192 && g.cap <= 8192) return 1;
+  int64_t target = g.B == 1 || tokens < (int64_t(1) << 20) ? 256 : tokens <= (int64_t(1) << 22) ? 512 : 1024;
+  const auto short_of = [&](int64_t t) { return t / BG * BG * 8 < t * 7; };
+  if (target == 256 && short_of(256)) target = 512;
+  int64_t S = target / BG + (target == 512 && short_of(512) ? 1 : 0);
   const int64_t most = units / (dense ? 2 : 4);
   if (S > most) S = most;
   if (S > 256) S = 256;

@@ -484,6 +484,13 @@ def test_many_groups():
     against_long([700 + i for i in range(40)], 40, 8, 2, 64, 64, BF, "step")
 
 
+@pytest.mark.parametrize("kind", ["dense", "step"])
+@pytest.mark.parametrize("B,Hkv,T", [(25, 8, 2500), (3, 8, 6001), (20, 5, 3500), (32, 6, 9000)])
+def test_groups_of_each_plan(kind, B, Hkv, T):
+    """Groups enough for one workgroup each, and numbers of them that divide no number of workgroups."""
+    against_long([max(0, T - 131 * i) for i in range(B)], B, Hkv, 1, 128, 64, BF, kind)
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 4 GiB of keys: its last pages stored, indexed, copied and read."""
     Hkv, d, page, P = 8, 128, 128, 40000
