@@ -302,6 +302,7 @@ struct IndexArgs {
   float* mx;
   PageGeom pg;
   int max_new;
+  unsigned run, runs, rounds;    // neighbours of a run, runs of a (sequence, kv head), rounds along x
 };
 
 // fp32 -> E4M3, nearest even, saturating at 448; NaN stays
@@ -319,11 +320,17 @@ __global__ __launch_bounds__(256, 2) void page_summaries_kernel(IndexArgs a) {
   __shared__ float mx_s[NB];
   __shared__ bool there_s[NB];
   const Geom& g = a.pg.g;
-  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int col = lane & 15, g4 = lane >> 4;
-  // workgroups go to the XCDs round robin: each XCD takes a run of neighbours, whose records
-  // share cache lines
-  const int per = gridDim.x / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  // Workgroups go to the XCDs round robin.  Each XCD takes runs of neighbours, whose records share
+  // cache lines (at most eight runs of a sequence and head; 130K tokens 38.5 us in eight, 40.8 in
+  // 64), and the runs of all sequences and heads are dealt to the XCDs in turn (with every one's
+  // first run on the first XCD, short ones left the others idle: 64 times 9 blocks of 128 tokens
+  // 11.2 us, so 8.1; one block each of 128 heads 7.3, 5.0).
+  const unsigned i8 = blockIdx.x >> 3, r = (i8 / a.run + blockIdx.y * a.rounds) * 8 + (blockIdx.x & 7);
+  const unsigned bh = r / a.runs, at = r % a.runs * a.run + i8 % a.run;
+  if (bh >= (unsigned)(g.B * g.Hkv)) return;
+  const int b = bh / g.Hkv, h = bh % g.Hkv;
   int64_t N = clamp_len(a.seq_lens, b, g.cap) / BS, j0 = (int64_t)at * NB;
   if (N > g.ncap) N = g.ncap;
   if (a.prev_lens != nullptr) {
@@ -855,7 +862,6 @@ hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool
   const int64_t most = g.cap / g.BS < g.ncap ? g.cap / g.BS : g.ncap;
   const int64_t nblk = prev_lens != nullptr && max_new < most ? max_new : most;
   if (nblk <= 0) return hipSuccess;
-  const IndexArgs a{(const uint8_t*)pool.k, pool.k_scale, table, prev_lens, seq_lens, s.mu, s.sigma, s.max_norm, pg, max_new};
   // Large caches (past what the last-level cache holds): 32 blocks to a workgroup, whose records
   // leave as whole rows, the keys read past the caches.  Below, one block to a wavefront, four to a
   // workgroup, so that as many start as there are.  us with 32 and the hint / 4 without, fp32
@@ -863,7 +869,12 @@ hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool
   // (64 x 64) 114 / 119; 98 MiB (128 x 64) 33 / 29; 49 MiB (64 x 128) 20 / 14; 4 MiB 23 / 7.
   const bool large = nblk >= 32 && nblk * g.Hkv * g.B * g.BS * g.D > (int64_t(200) << 20);
   const int nb = large ? 32 : 4;
-  const dim3 grid((unsigned)((nblk + 8 * nb - 1) / (8 * nb) * 8), g.Hkv, g.B);
+  const unsigned wgs = (unsigned)((nblk + nb - 1) / nb), runs = wgs < 64 ? (wgs + 7) / 8 : 8, run = (wgs + runs - 1) / runs;
+  const int64_t rounds = ((int64_t)g.B * g.Hkv * runs + 7) / 8, most_x = run < 16 ? 65536 : (1 << 20) / run,
+                along = rounds < most_x ? rounds : most_x;
+  const IndexArgs a{(const uint8_t*)pool.k, pool.k_scale, table, prev_lens, seq_lens, s.mu, s.sigma, s.max_norm, pg, max_new,
+                    run, runs, (unsigned)along};
+  const dim3 grid((unsigned)along * 8 * run, (unsigned)((rounds + along - 1) / along));
   return with_hook(hook, ETA_KERNEL_PAGE_SUMMARIES, stream, [&] {
 #define ETA_PSUM(D_, BS_)                                                                                    \
   if (g.D == D_ && g.BS == BS_) {                                                                            \

@@ -185,6 +185,20 @@ def test_index_large():
     assert not a.max_norm[..., n - 1:].any() and a.max_norm[..., :n - 1].all()
 
 
+def test_index_of_a_million_groups():
+    """More (sequence, kv head) groups than one dimension of the grid takes."""
+    gen = torch.Generator().manual_seed(2)
+    pool = filled(gen, 1, 16, 64, 64)
+    B = 65535
+    out = eta.build_page_summaries(pool, torch.zeros(B, 1, dtype=torch.int32, device="cuda"),
+                                   torch.full((B,), 64, dtype=torch.int32, device="cuda"), stat_dtype=E4M3)
+    one = eta.build_page_summaries(pool, ints(0).view(1, 1), ints(64), stat_dtype=E4M3)
+    for name in ("mu", "sigma", "max_norm"):
+        a, b = (getattr(x, name) for x in (out, one))
+        a, b = (x.view(torch.uint8) if x.dtype == E4M3 else x for x in (a, b))
+        assert (a == b).all() and b.any(), name
+
+
 # ---------------------------------------------------------------- decode
 
 class Case:
