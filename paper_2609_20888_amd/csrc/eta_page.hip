@@ -867,7 +867,10 @@ hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool
   // workgroup, so that as many start as there are.  us with 32 and the hint / 4 without, fp32
   // records: 256 MiB of keys (128 x 128 blocks) 57 / 69; 469 MiB (128 dims x 64) 111 / 117, 469 MiB
   // (64 x 64) 114 / 119; 98 MiB (128 x 64) 33 / 29; 49 MiB (64 x 128) 20 / 14; 4 MiB 23 / 7.
-  const bool large = nblk >= 32 && nblk * g.Hkv * g.B * g.BS * g.D > (int64_t(200) << 20);
+  // Between, four with the hint: 127 MiB (128 x 64) 39.1 without, 35.2 with it, 146 MiB 41.5 / 39.0, 128
+  // MiB of different lengths 30.9 / 31.3; below, keys just stored are still in the caches.
+  const int64_t keys = nblk * g.Hkv * g.B * g.BS * g.D;
+  const bool large = nblk >= 32 && keys > (int64_t(200) << 20), hint = keys > (int64_t(96) << 20);
   const int nb = large ? 32 : 4;
   const unsigned wgs = (unsigned)((nblk + nb - 1) / nb), runs = wgs < 64 ? (wgs + 7) / 8 : 8, run = (wgs + runs - 1) / runs;
   const int64_t rounds = ((int64_t)g.B * g.Hkv * runs + 7) / 8, most_x = run < 16 ? 65536 : (1 << 20) / run,
@@ -880,6 +883,8 @@ hipError_t launch_page_summaries(const PageGeom& pg, const eta_page_pool_t& pool
   if (g.D == D_ && g.BS == BS_) {                                                                            \
     if (large)                                                                                               \
       hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, 32, true>), grid, dim3(256), 0, stream, a);         \
+    else if (hint)                                                                                           \
+      hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, 4, true>), grid, dim3(256), 0, stream, a);          \
     else                                                                                                     \
       hipLaunchKernelGGL((page_summaries_kernel<D_, BS_, 4, false>), grid, dim3(256), 0, stream, a);         \
   }

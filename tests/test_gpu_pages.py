@@ -185,6 +185,24 @@ def test_index_large():
     assert not a.max_norm[..., n - 1:].any() and a.max_norm[..., :n - 1].all()
 
 
+@pytest.mark.parametrize("Hkv,d,page", [(1, 64, 64), (2, 128, 128)])
+def test_index_middle(Hkv, d, page):
+    """A cache between the sizes that fit the caches and the largest, against its parts."""
+    n = (100 << 20) // (Hkv * d * page) + 3
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    codes = torch.randint(0, 0x7f, (n, Hkv, page, d), generator=gen, dtype=torch.uint8, device="cuda").view(E4M3)
+    pool = eta.PagePool(codes, codes.view(n, Hkv, d, page), torch.full((n, Hkv), 0.02, device="cuda"), torch.ones(n, Hkv, device="cuda"))
+    table = torch.randperm(n, generator=gen, device="cuda").int().view(1, n)
+    lens = ints(n * page - 5)
+    a = eta.build_page_summaries(pool, table, lens)
+    b = eta.Summaries.empty(1, Hkv, d, n, "cuda")
+    for j in range(0, n, 2000):
+        eta.update_page_summaries(pool, table, ints(j * page), lens, b, max_new_blocks=2000)
+    for name in ("mu", "sigma", "max_norm"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+    assert not a.max_norm[..., n - 1:].any() and a.max_norm[..., :n - 1].all()
+
+
 def test_index_of_a_million_groups():
     """More (sequence, kv head) groups than one dimension of the grid takes."""
     gen = torch.Generator().manual_seed(2)
