@@ -625,9 +625,9 @@ eta_status_t eta_page_summaries(const eta_page_desc_t* pd, const eta_page_pool_t
  * pages: the same screening, thresholds, rescue, results and parameters, K and V being what the
  * pages hold.  Lengths are clamped to [0, min(table_blocks*b, n_blk_cap*b + b - 1)], so the
  * index may leave out a last block that is never full.  Products on the matrix cores from
- * operands that hold the codes and bf16 queries exactly (fp32 queries in three bf16 parts) and
- * the softmax weights in two (three) bf16 parts; sums and statistics in fp32.  num_splits counts
- * the workgroups of every (sequence, kv head) (0: the library's choice, by the sizes).
+ * operands that hold the codes, the queries and the softmax weights exactly (what has 24 bits in
+ * three bf16 parts); sums and statistics in fp32.  num_splits counts the workgroups of every
+ * (sequence, kv head) (0: the library's choice, by the sizes).
  *   workspace   >= eta_page_decode_workspace_size() bytes, 256-byte aligned
  */
 eta_status_t eta_page_decode_workspace_size(const eta_page_desc_t* pd, int64_t n_blk_cap,

@@ -18,10 +18,11 @@
 // has its own, and they are merged once at the end.  The contraction runs in the order the loads
 // give (any order does that both operands share).
 //
-// The weights go to p.V as two bf16 parts (16 bits), and fp32 queries as three with weights of
-// three: the time of the matrix cores does not bound these kernels.  One part would add 2^-9 of
-// each weight, as much as the bf16 output's own rounding; fp16 would lose weights below 2^-24,
-// which a long context has many of beside one that stands out.
+// The weights go to p.V as three bf16 parts, which keep all 24 bits, and fp32 queries to the scores as
+// three too.  Two parts (16 bits) would be 2^-18 of a weight off, more than fp32 sums are: where weights
+// nearly cancel that shows in bf16 outputs too, and one in a thousand of a long context's rounds the
+// other way.  Two / three parts, us in a graph: 512K tokens 73.3 / 73.5, 16 x 64K 76.8 / 77.4, dense 8 x
+// 32K 40.9 / 41.6, 16 x 3400 of 64 dims in groups of eight 19.2 / 19.8.
 //
 // Bound by HBM once the caches are long: without the gate, the softmax and p.V the same loads take
 // the same time.  512K tokens, 4 kv heads, d = 128, 283.7 MB of a step's union: 48.4 us (5.9 TB/s; a
@@ -139,7 +140,7 @@ struct Column {
 template <int D, bool DENSE, bool F32, int REP>
 struct Attend {
   static constexpr int NQ = F32 ? 3 : 1;     // bf16 parts of the queries
-  static constexpr int NP = F32 ? 3 : 2;     // and of the weights
+  static constexpr int NP = 3;               // and of the weights
   static constexpr int NC = D / 32;          // steps of a score's contraction
   static constexpr int TS = 4 / REP;         // tiles of a replica
   static constexpr int NS = 4 * TS;          // scores of a lane

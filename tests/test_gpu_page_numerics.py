@@ -1,0 +1,75 @@
+"""What the paged cache's kernels round, looked at where a coarser rounding would show: weights that
+nearly cancel; needs an MI355X."""
+import math
+
+import pytest
+import torch
+
+import page_support as ps
+from gpu_support import require_gpu, say
+from page_support import BF, E4M3, F32, F64, I32
+from paper_2609_20888_amd import eta
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _gpu(request):
+    require_gpu()
+    say(f"\n[gpu] {request.node.nodeid}")
+    yield
+    torch.cuda.synchronize()
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=I32, device="cuda")
+
+
+def pool_of(k, v):
+    """A pool of pages k, v [P][Hkv][page][d] of values that are codes, with scales of 1."""
+    one = torch.ones(k.shape[:2], device="cuda")
+    return eta.PagePool(k.cuda().to(E4M3), v.transpose(2, 3).contiguous().cuda().to(E4M3), one, one.clone())
+
+
+# ---------------------------------------------------------------- the softmax weights
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,page,G", [(64, 64, 1), (128, 64, 8), (64, 128, 2), (128, 128, 4)])
+def test_weights_keep_24_bits(d, page, G, dtype):
+    """Two tokens of nearly equal weight and opposite values beside a third one: what is left of
+    them is 2^-13 of either, and as far off as the weights' own rounding.
+
+    Scores are sums of two exact products.  A weight 2^x, |x| < 1.1, is off by at most 2^-23 (the
+    exponential) + 2^-24 (x, formed and shifted in 32 bits) + 2^-25 (its three parts) relative, the
+    two sums it enters by 2^-24 each: 2^-21 of sum p |v| in all.  (Weights of 16 bits: 2^-18.)"""
+    gen = torch.Generator().manual_seed(d + page + G)
+    B, Hkv, n = 16, 2, 3
+    Hq, T = G * Hkv, [page * 2 + 9 - i for i in range(B)]
+    q = torch.zeros(B, Hq, d)
+    q[..., 0] = ((0.3 + 0.4 * torch.rand(B, Hq, generator=gen)) * math.sqrt(d)).to(BF).float()
+    q[..., 1] = 2.0 ** -13 * math.sqrt(d) if d == 64 else 2.0 ** -10
+    k, v = torch.zeros(B * n, Hkv, page, d), torch.zeros(B * n, Hkv, page, d)
+    k[..., 0] = -448.0                                                # every other token: a weight of zero
+    for b in range(B):
+        for h in range(Hkv):
+            at = torch.randperm(T[b], generator=gen)[:3].tolist()
+            x = torch.exp2(torch.randint(-3, 4, (d,), generator=gen).float())
+            for t, key, val in zip(at, ((-1, 0), (-1, -1), (0, 0)), (x, -x, 0 * x)):
+                p, i = b * n + t // page, t % page
+                k[p, h, i, :2], v[p, h, i] = torch.tensor(key, dtype=F32), val
+    pool, table, lens = pool_of(k, v), torch.arange(B * n, dtype=I32).view(B, n).cuda(), ints(*T)
+    kk, vv = (x.view(B, n, Hkv, page, d).transpose(1, 2).reshape(B, Hkv, n * page, d).double() for x in (k, v))
+    summ = eta.build_page_summaries(pool, table, lens)
+    for splits in (0, 1, 3):
+        outs = (eta.dense_decode_pages(q.to(dtype).cuda(), pool, table, lens, num_splits=splits),
+                eta.decode_pages(q.to(dtype).cuda(), pool, table, lens, summ, torch.full((B, Hq), -math.inf, device="cuda"),
+                                 params=eta.decode_params(beta=4.0, num_splits=splits)).out)
+        for b in range(B):
+            for r in range(Hq):
+                p = torch.softmax(kk[b, r // G, :T[b]] @ q[b, r].double() / math.sqrt(d), 0)
+                want, mass = p @ vv[b, r // G, :T[b]], p @ vv[b, r // G, :T[b]].abs()
+                tol = 2.0 ** -21 * mass
+                tol = tol + ps.half_step(dtype) * (want.abs() + tol)
+                for out in outs:
+                    worst = ((out[b, r].cpu().double() - want).abs() - tol).max().item()
+                    assert worst <= 0, (b, r, splits)
