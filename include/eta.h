@@ -623,8 +623,8 @@ eta_status_t eta_page_summaries(const eta_page_desc_t* pd, const eta_page_pool_t
 /*
  * eta_page_decode, eta_page_decode_predicted -- eta_decode and eta_decode_predicted over the
  * pages: the same screening, thresholds, rescue, results and parameters, K and V being what the
- * pages hold.  Lengths are clamped to [0, min(table_blocks*b, n_blk_cap*b + b - 1)], so the
- * index may leave out a last block that is never full.  Products on the matrix cores from
+ * pages hold.  n_blk_cap >= table_blocks - 1: the index may leave out a table's last block where
+ * it is never full (lengths are clamped to [0, min(table_blocks*b, n_blk_cap*b + b - 1)]).  Products on the matrix cores from
  * operands that hold the codes, the queries and the softmax weights exactly (what has 24 bits in
  * three bf16 parts); sums and statistics in fp32.  num_splits counts the workgroups of every
  * (sequence, kv head) (0: the library's choice, by the sizes).

@@ -104,10 +104,14 @@ eta_status_t check_groups(const Geom& g) {
   return ETA_OK;
 }
 
-// The decode's geometry: no sequence holds more full blocks than the index.
+// The decode's geometry: the index has room for every full block, but for a table's last one, which a
+// caller that never fills it may leave out.
 eta_status_t set_decode(int64_t n_blk_cap, Geom* g) {
   if (eta_status_t st = check_groups(*g)) return st;
   if (eta_status_t st = set_index(n_blk_cap, g)) return st;
+  if (n_blk_cap < g->cap / g->BS - 1)
+    return fail(ETA_ERR_INVALID_ARG, "n_blk_cap (%lld) < table_blocks - 1 (%lld)", (long long)n_blk_cap,
+                (long long)(g->cap / g->BS - 1));
   const int64_t most = n_blk_cap * g->BS + g->BS - 1;
   if (g->cap > most) g->cap = most;
   return ETA_OK;

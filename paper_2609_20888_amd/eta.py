@@ -1153,7 +1153,8 @@ def decode_pages(q: torch.Tensor, pool: PagePool, table: torch.Tensor, seq_lens:
                  union_counts=None, want_counts: bool = True, workspace: Optional[torch.Tensor] = None,
                  stream=None) -> DecodeOut:
     """eta_page_decode: one ETA decode step over pages (decode's results; q [B][Hq][d], table int32
-    [B][blocks], summ as build_page_summaries gives it, tau fp32 [B][Hq])."""
+    [B][blocks], summ as build_page_summaries gives it, tau fp32 [B][Hq]).  The index needs a record
+    for every block of the table but the last, and that one's too where it is ever full."""
     if tau is None:
         raise ValueError("tau must be given")
     return _decode_pages(q, pool, table, seq_lens, summ, tau, None, None, params, out, mask, counts, union_counts, None,

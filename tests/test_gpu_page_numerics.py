@@ -1,5 +1,5 @@
 """What the paged cache's kernels round, looked at where a coarser rounding would show: weights that
-nearly cancel; needs an MI355X."""
+nearly cancel; an index at the least size; needs an MI355X."""
 import math
 
 import pytest
@@ -9,6 +9,7 @@ import page_support as ps
 from gpu_support import require_gpu, say
 from page_support import BF, E4M3, F32, F64, I32
 from paper_2609_20888_amd import eta
+from test_gpu_pages import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +74,22 @@ def test_weights_keep_24_bits(d, page, G, dtype):
                 for out in outs:
                     worst = ((out[b, r].cpu().double() - want).abs() - tol).max().item()
                     assert worst <= 0, (b, r, splits)
+
+
+# ---------------------------------------------------------------- an index of one block less
+
+@pytest.mark.parametrize("splits", [0, 1, 3])
+@pytest.mark.parametrize("page", [64, 128])
+def test_index_of_one_block_less_than_the_table(page, splits):
+    """A table whose last block is never full, with no record for it; lengths past it count up to it."""
+    c = Case(3, 2, 4, 64, page, [page * 7 - 1, page * 6, page * 6 + 1], BF, cap=7)
+    short = eta.Summaries.empty(3, 2, 64, 6, "cuda")
+    eta.build_page_summaries(c.pool, c.table.cuda(), ints(*c.lens), out=short)
+    for name in ("mu", "sigma", "max_norm"):
+        assert torch.equal(getattr(short, name), getattr(c.summ, name)[..., :6])
+    c.summ = short
+    c.check(c.run(num_splits=splits))
+    want = c.run(num_splits=splits)
+    c.lens[0] = 10 ** 6
+    got = c.run(num_splits=splits)
+    assert torch.equal(got.out, want.out) and torch.equal(got.counts, want.counts)
