@@ -663,7 +663,8 @@ typedef struct {
   int32_t batch;               /* rows, <= 65535 */
   int32_t block_size;          /* tokens of a page, >= 1 */
   int64_t num_pages;           /* < 2^31 */
-  int64_t table_blocks;        /* entries of a row, >= 1; table_blocks * block_size < 2^31 */
+  int64_t table_blocks;        /* entries of a row, >= 1; table_blocks * block_size < 2^31 and
+                                  batch * table_blocks < 2^31 */
   int64_t table_stride;        /* elements between rows of every table of the call, >= table_blocks */
 } eta_table_desc_t;
 

@@ -228,6 +228,9 @@ eta_status_t check_table(const eta_table_desc_t* td) {
   if (td->table_stride < td->table_blocks || td->table_stride >= (int64_t(1) << 40))
     return fail(ETA_ERR_INVALID_ARG, "table_stride (%lld) < table_blocks (%lld)", (long long)td->table_stride,
                 (long long)td->table_blocks);
+  // (lacking entries, their ranks and a page's holders are counted in 32 bits)
+  if (td->batch * td->table_blocks >= (int64_t(1) << 31))
+    return fail(ETA_ERR_UNSUPPORTED, "batch * table_blocks must be below 2^31");
   return ETA_OK;
 }
 
