@@ -60,10 +60,32 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
+
+// A page may hold any scale (one coded elsewhere by amax / 448).  With one that is no power of two a
+// quotient x / scale, or a product of a code and the ratio of two scales, can round to the middle between
+// two codes that it only lies next to, and the tie would go to the wrong one.  So both are rounded to odd:
+// y, the nearest to the exact value, with the sign of what that leaves in `rest`, becomes the one of its
+// two neighbours in 32 bits whose last bit is set, which rounds to a code as the exact value does.
+__device__ __forceinline__ float to_odd(float y, float rest) {
+  if (!(rest < 0.f || rest > 0.f)) return y;         // (exact, or not finite)
+  const uint32_t u = __float_as_uint(y), beyond = (u ^ __float_as_uint(rest)) >> 31;
+  return __uint_as_float((u - beyond) | 1u);
+}
+// x / scale for a scale that is no power of two, as it is coded.  (`up` keeps the rest above the least float.)
+__device__ __forceinline__ float quotient(float x, float scale) {
+  const float up = scale < 0x1p-60f ? 0x1p64f : 1.0f, y = (x * up) / (scale * up);
+  return to_odd(y, fmaf(-y, scale * up, x * up));
+}
+__device__ __forceinline__ bool is_power_of_two(float s) { return (__float_as_uint(s) & 0x7fffffu) == 0; }
+
 // the codes of a word times r, rounded again
 __device__ __forceinline__ uint32_t scaled4(uint32_t w, float r) {
   const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-  return pack4(lo[0] * r, lo[1] * r, hi[0] * r, hi[1] * r);
+  auto times = [r](float c) {
+    const float y = c * r;
+    return to_odd(y, fmaf(c, r, -y));
+  };
+  return pack4(times(lo[0]), times(lo[1]), times(hi[0]), times(hi[1]));
 }
 
 // Eight elements of a row in 32 bits.
@@ -149,7 +171,15 @@ __global__ __launch_bounds__(D / 8 * (BS / 4)) void page_store_kernel(StoreArgs 
   // (a scale held that is no power of two, or NaN, is kept where it is not less)
   const bool grows = lo == 0 || need > held;
   const float scale = grows ? need : held;
-  const float inv = grows ? power_of_two(-e2) : 1.0f / held, again = held / scale;
+  float inv = grows ? power_of_two(-e2) : 1.0f / held;
+  const float again = held / scale;
+  if (!grows && !is_power_of_two(held)) {            // (the whole workgroup)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[r][e] = quotient(x[r][e], held);
+    inv = 1.0f;
+  }
   const bool round_held = lo > 0 && grows;
   if (tid == 0 && grows) a.scale[kv][si] = scale;
   if (kv == 0) {
@@ -229,7 +259,12 @@ __global__ __launch_bounds__(256) void page_token_kernel(StoreArgs a) {
   const int e2 = scale_exponent(wave_max64(amax));
   const float need = power_of_two(e2);
   const bool grows = lo == 0 || need > held;
-  const float inv = grows ? power_of_two(-e2) : 1.0f / held;
+  float inv = grows ? power_of_two(-e2) : 1.0f / held;
+  if (!grows && !is_power_of_two(held)) {
+#pragma unroll
+    for (int e = 0; e < PL; ++e) x[e] = quotient(x[e], held);
+    inv = 1.0f;
+  }
   if (lo > 0 && grows) {
     const float again = held / need;
     for (int k = tid; k < BS * D / 16; k += 256) {
