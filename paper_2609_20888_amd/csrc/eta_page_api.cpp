@@ -117,38 +117,52 @@ eta_status_t set_decode(int64_t n_blk_cap, Geom* g) {
   return ETA_OK;
 }
 
-// Splits per (sequence, kv head), each a workgroup; 0: the proportional plan.  256 workgroups in all
-// (one a compute unit, of the two that fit at once), 512 for batches of a million tokens and more
-// over the kv heads, 1024, whose order evens out different lengths, past 2^22.  Not more than that (a
-// few left over take as long as a whole round: dense, 3 x 21K tokens, 8 kv heads 504 / 528: 26.8 / 37.5
-// us) unless an eighth of them would be missing: then 512 (100 groups of 6000 tokens 300 / 500: 29.5 /
-// 27.7), or one more split (192 groups of 16K tokens 384 / 576: 83 / 74).  us by workgroups in all, 128 dims: dense, 2 x 8000 tokens, 4 kv heads 128 / 256 / 512:
-// 11.8 / 10.7 / 13.6; 8 x 8000, 8 heads 32.4 / 24.4 / 24.9; 8 x 32K, 4 heads 256 / 512 / 1024 39.1 /
-// 38.2 / 38.7; a step of 2 x 158K, 2 heads 22.9 / 26.1 / 37.9, 16 x 16K, 8 heads 57.3 / 55.4 / 55.7, 16 x
-// 64K 166 / 161 / 152, of 512K tokens 128 / 256: 95 / 69.  A workgroup alone on a small share waits for
-// its own loads (1000 tokens in one: 12.0, in eight: 9.4).
-// The proportional plan deals workgroups by the lengths (or unions) that the kernel finds, at 2 to
-// 3 us: where equal shares would leave more than 64 units of 64 tokens (a step, which reads a part
-// of them: 128) of the longest sequence to one workgroup.
-// One workgroup of eight wavefronts for each writes the results itself, a launch less: where the
-// groups alone fill the card and are not long (a step of 32 x 4000, 8 heads: 33.0 / in two 37.8; dense
-// 35.4 / 40.9; 24 x 4000 31.9 / 35.6; equal at 16K), and for the smallest calls, whose launches the
-// host takes 4 us for (dense, 2 x 1500 tokens of 64 dims: 10.4 us in a graph against 8.9, but 11
-// against 13 launched one by one; a step of 4000: 13.6 against 14.5, and 20 against 23).
+// Splits per (sequence, kv head), each a workgroup; 0: the proportional plan.  By the bytes of the codes
+// that the capacity holds (of which a step reads a part: an eighth counts where what is read does), each
+// border where the two sides cross over 3300 sizes in graphs (128 to 512K tokens of 1 to 512 groups, both
+// head dims, page sizes and query types, group sizes 1, 4 and 8; equal lengths, lengths n / 4 .. n and
+// lengths of all magnitudes), all within 1 to 4% of the fastest plan in the mean.
+//
+// One workgroup of eight wavefronts for a group writes the result itself, a launch and its merge less.
+// Few groups: dense up to about 1000 tokens of 64 dims or 500 of 128 (one / split, us of the fastest:
+// 512 tokens of 64 dims 0.83, 2048 1.35; 128 dims 256 0.95, 1024 1.46); a step, whose share of blocks grows
+// with the heads of a group, up to 2500 of 64 dims and G = 4 (1024 0.95, 4096 1.15; G = 8, 128 dims: 540
+// tokens 28.8 / 23.5 us).  The more groups, the less the rest of the card can take off them: 128 groups
+// 4000 and 1300 tokens dense, from 200 groups on one stays faster up to a million elements of K, a step's
+// up to two (192 groups of 9700 tokens of 128 dims: 48.8 / 55.7).
+//
+// Else 256 workgroups in all, one a compute unit of the two that fit at once.  Batches are of different
+// lengths, and 512 even them out: dense from 48 MiB (64 MiB of 16 groups, 256 / 512: equal lengths 1.00 /
+// 1.05, n / 4 .. n 1.03 / 1.01, all magnitudes 1.19 / 1.01), a step from 192 MiB, and from 1.5 GiB 1024 (2
+// GiB of 100 and more groups, 512 / 1024: 1.05 / 1.02, 1.07 / 1.04, 1.20 / 1.08).  Not more than that (a few left
+// over take as long as a whole round: dense, 3 x 21K tokens, 8 kv heads 504 / 528: 26.8 / 37.5 us) unless
+// an eighth of them would be missing: then 512 (100 groups of 6000 tokens 300 / 500: 29.5 / 27.7), or one
+// more split (192 groups of 16K tokens 384 / 576: 83 / 74).  A merge takes longer the more splits it
+// reads: of one group 64 below 12 MiB read (dense, 2 MiB 64 / 256: 1.01 / 1.44), 128 below 48 MiB (16 MiB 64 /
+// 128 / 256: 1.21 / 1.00 / 1.16).
+//
+// The proportional plan deals workgroups by the lengths (or unions) that the kernel finds, at 2 to 3 us:
+// dense from 192 MiB and 12 groups on (512 MiB of 64 groups, 512 / dealt: equal 1.02 / 1.03, n / 4 .. n 1.11 /
+// 1.00, all magnitudes 1.51 / 1.02; below 12 groups its 512 workgroups are too many), a step from 768 MiB and
+// for at most 96 groups, whose counts every workgroup reads (1 GiB of 64 to 100 groups, 512 / dealt:
+// 1.01 / 1.06, 1.04 / 1.03, 1.15 / 1.05; of more 1.06 / 1.10, 1.03 / 1.08, 1.06 / 1.01).
 int page_plan(const Geom& g, bool dense) {
-  if (dense ? g.cap * g.D <= 1536 * 64 : g.cap * g.D * g.G <= 6000 * 64) return 1;
-  const int64_t BG = (int64_t)g.B * g.Hkv, units = (g.cap + 63) / 64, tokens = BG * g.cap;
-  if (BG >= 192 && g.cap <= 8192) return 1;
-  int64_t target = g.B == 1 || tokens < (int64_t(1) << 20) ? 256 : tokens <= (int64_t(1) << 22) ? 512 : 1024;
+  const int64_t BG = (int64_t)g.B * g.Hkv, units = (g.cap + 63) / 64, keys = g.cap * g.D, MiB = int64_t(1) << 20;
+  const double idle = BG < 256 ? 1.0 - BG / 256.0 : 0.0, alone = idle * std::sqrt(idle);
+  if (dense ? keys <= 1.1e6 && keys * alone <= 60e3 : keys <= 2.2e6 && keys * alone * (g.G > 2 ? g.G : 2) <= 640e3) return 1;
+  const int64_t group = 2 * keys, total = BG * group, read = group / (dense ? 1 : 8);
+  const bool dealt = dense ? BG <= kPropMaxGroups && BG * (units + 2) < (int64_t(1) << 30)
+                           : BG <= 96 && BG * g.n_tiles <= kPropMaxCounts;
+  if (g.B > 1 && BG >= 12 && dealt && total >= (dense ? 192 : 768) * MiB) return 0;
   const auto short_of = [&](int64_t t) { return t / BG * BG * 8 < t * 7; };
-  if (target == 256 && short_of(256)) target = 512;
+  int64_t target = 256;
+  if (short_of(256) || (g.B > 1 && total >= (dense ? 48 : 192) * MiB)) target = 512;
+  if (!dense && g.B > 1 && total >= 1536 * MiB) target = 1024;
   int64_t S = target / BG + (target == 512 && short_of(512) ? 1 : 0);
-  const int64_t most = units / (dense ? 2 : 4);
-  if (S > most) S = most;
-  if (S > 256) S = 256;
-  if (S < 1) S = 1;
-  const bool dealt = BG <= kPropMaxGroups && (dense ? BG * (units + 2) < (int64_t(1) << 30) : BG * g.n_tiles <= kPropMaxCounts);
-  return g.B > 1 && dealt && units > S * (dense ? 64 : 128) ? 0 : (int)S;
+  const int64_t most = units / (dense ? 2 : 4), merged = read < 12 * MiB ? 64 : read < 48 * MiB ? 128 : 256;
+  S = S < most ? S : most;
+  S = S < merged ? S : merged;
+  return S < 1 ? 1 : (int)S;
 }
 
 SplitPlan page_splits(const Geom& g, int num_splits) {
