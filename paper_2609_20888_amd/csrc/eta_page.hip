@@ -323,8 +323,8 @@ __global__ __launch_bounds__(256) void page_token_kernel(StoreArgs a) {
 // The block stays in registers for both passes (two passes: mean first, so that a coordinate
 // whose mean is far larger than its spread loses nothing).  Results are staged in LDS and leave
 // as rows of the dimension-major records.  (NaN times a zero of the unit matrix is NaN: a key with
-// NaN makes the means and deviations of the 32 dims beside it NaN too; the block's bound is NaN
-// with one of them.)
+// NaN makes the means and deviations of the 32 dims of its step NaN too, and may leave the norms of
+// other tokens out; the block's bound is NaN with one of them.)
 
 struct IndexArgs {
   const uint8_t* k;

@@ -93,3 +93,49 @@ def test_index_of_one_block_less_than_the_table(page, splits):
     c.lens[0] = 10 ** 6
     got = c.run(num_splits=splits)
     assert torch.equal(got.out, want.out) and torch.equal(got.counts, want.counts)
+
+
+# ---------------------------------------------------------------- keys of NaN in the index
+
+@pytest.mark.parametrize("rec", [F32, torch.float16, E4M3])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 64), (64, 128), (128, 128)])
+def test_a_key_of_nan_makes_its_block_s_bound_nan(d, page, rec):
+    """One code of NaN at every place of a 16 x 32 tile and at the ends of rows and blocks: the bounds of
+    that block and head are NaN, which selects nothing; every other record as before, and of its own
+    block those of all but the 32 dimensions that share its products (alternate eights of 64)."""
+    places = [(t, i) for t in (0, 1, 5, 15) for i in (0, 17, 31)] + [(page - 1, d - 1), (page // 2, d // 2), (3, d - 32), (page - 2, 1)]
+    B, Hkv, n, G = 2, 2, len(places) + 1, 4
+    gen = torch.Generator().manual_seed(d + page)
+    k = torch.randint(0, 0x70, (B * n, Hkv, page, d), generator=gen, dtype=torch.uint8)
+    k += 128 * torch.randint(0, 2, k.shape, generator=gen, dtype=torch.uint8)
+    ks = 2.0 ** torch.randint(-9, -5, (B * n, Hkv), generator=gen).float()
+    table = torch.randperm(B * n, generator=gen).view(B, n).to(I32)
+    v = torch.zeros(B * n, Hkv, d, page, dtype=torch.uint8)
+    lens, q = ints(n * page, n * page), torch.randn(B, G * Hkv, d, generator=gen).to(BF).cuda()
+
+    def run(k):
+        pool = eta.PagePool(k.cuda().view(E4M3), v.cuda().view(E4M3), ks.cuda(), torch.ones_like(ks).cuda())
+        s = eta.build_page_summaries(pool, table.cuda(), lens, stat_dtype=rec)
+        like = torch.empty(B, Hkv, n * page, d, dtype=BF, device="cuda")       # (a contiguous cache of these sizes)
+        bounds = eta.block_bounds(q, lens, s, like, block_size=page, z=1.0)
+        tau = torch.full((B, G * Hkv), -1e30, device="cuda")
+        got = eta.decode_pages(q, pool, table.cuda(), lens, s, tau, params=eta.decode_params(rescue_window=0))
+        return [x.float().cpu() for x in (s.mu, s.sigma, s.max_norm, bounds)], got.mask.cpu()
+    want, every = run(k)
+    assert every.all() and not want[3].isnan().any()
+    nan = k.clone()
+    for j, (t, i) in enumerate(places):
+        nan[int(table[1, j]), 1, t, i] = 0x7f if j % 2 else 0xff
+    got, mask = run(nan)
+    on = torch.ones(B, Hkv, n, dtype=torch.bool)
+    on[1, 1, :len(places)] = False
+    heads = on.repeat_interleave(G, 1)
+    assert torch.equal(mask.bool(), heads) and torch.equal(got[3].isnan(), ~heads)
+    assert torch.equal(got[3][heads], want[3][heads]) and torch.equal(got[2][on], want[2][on])
+    for a, b in zip(got[:2], want[:2]):
+        x = on[:, :, None].expand_as(a)
+        assert torch.equal(a[x], b[x])
+        for j, (_, i) in enumerate(places):
+            assert a[1, 1, i, j].isnan()
+            far = torch.tensor([(c // 64, c // 8 % 2) != (i // 64, i // 8 % 2) for c in range(d)])
+            assert torch.equal(a[1, 1, far, j], b[1, 1, far, j]) and int(a[1, 1, :, j].isnan().sum()) <= 32
