@@ -628,6 +628,9 @@ eta_status_t eta_page_summaries(const eta_page_desc_t* pd, const eta_page_pool_t
  * operands that hold the codes, the queries and the softmax weights exactly (what has 24 bits in
  * three bf16 parts); sums and statistics in fp32.  num_splits counts the workgroups of every
  * (sequence, kv head) (0: the library's choice, by the sizes).
+ * Screening reads the index and not the table: a full block whose entry names no page is selected,
+ * rescued and counted (block_mask, head_token_counts, union_counts) by the records it has, and a
+ * last block's tokens are counted, though the outputs take nothing of either.
  *   workspace   >= eta_page_decode_workspace_size() bytes, 256-byte aligned
  */
 eta_status_t eta_page_decode_workspace_size(const eta_page_desc_t* pd, int64_t n_blk_cap,
@@ -688,7 +691,10 @@ eta_status_t eta_page_extend(const eta_table_desc_t* td, int32_t* table, int32_t
  * takes it; each further one gets a page of its own and a copy to make.  Entries behind a row's
  * last block, and those of an empty row, are -1.  refs gains the new table's entries and loses
  * the old one's, so the pages that no row goes on with become free (and may be given out again
- * by the same call).
+ * by the same call).  refs has no say in who keeps a page: where another
+ * holder (a second row of the table, a list of shared beginnings) has a last block that is not
+ * full, the first row's next tokens are stored beside that holder's, whose codes are rounded
+ * again if the scale grows.  Holders beyond a row keep full blocks only, or copies.
  *   table, refs, seq_lens         as they were;  table_out, refs_out, seq_lens_out: the new ones
  *   src, dst  int32 [batch]: for each row the page to copy and its own new one, or -1, -1
  *   missing   int32 [1]: how many rows found no free page (their last block's entry is -1)

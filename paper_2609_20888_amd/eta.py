@@ -1154,7 +1154,8 @@ def decode_pages(q: torch.Tensor, pool: PagePool, table: torch.Tensor, seq_lens:
                  stream=None) -> DecodeOut:
     """eta_page_decode: one ETA decode step over pages (decode's results; q [B][Hq][d], table int32
     [B][blocks], summ as build_page_summaries gives it, tau fp32 [B][Hq]).  The index needs a record
-    for every block of the table but the last, and that one's too where it is ever full."""
+    for every block of the table but the last, and that one's too where it is ever full.  Blocks without
+    a page are screened and counted by their records, though nothing of them is attended."""
     if tau is None:
         raise ValueError("tau must be given")
     return _decode_pages(q, pool, table, seq_lens, summ, tau, None, None, params, out, mask, counts, union_counts, None,
@@ -1269,7 +1270,9 @@ def fork_pages(table: torch.Tensor, refs: torch.Tensor, seq_lens: torch.Tensor, 
     """eta_page_fork: row b of the new table goes on from row parents[b] of the present one (int32
     [B]; outside [0, B): empty).  Full pages are shared; a last page that is not full is copied for
     every row but the first that takes it (copy_pages makes the copies, for each layer's pool); the
-    pages that no row goes on with become free.  table, refs and seq_lens are left as they are."""
+    pages that no row goes on with become free.  The first row keeps its last page whatever refs says:
+    what else holds pages (a list of shared beginnings) should hold full ones, since that row's next
+    tokens are stored there.  table, refs and seq_lens are left as they are."""
     o = out
     _, ref, dev, nbytes = _table_plan(
         8, int(page), (table, o and o.table), (refs, o and o.refs),
