@@ -139,3 +139,22 @@ def test_a_key_of_nan_makes_its_block_s_bound_nan(d, page, rec):
             assert a[1, 1, i, j].isnan()
             far = torch.tensor([(c // 64, c // 8 % 2) != (i // 64, i // 8 % 2) for c in range(d)])
             assert torch.equal(a[1, 1, far, j], b[1, 1, far, j]) and int(a[1, 1, :, j].isnan().sum()) <= 32
+
+
+# ---------------------------------------------------------------- the index's deviations
+
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 64), (64, 128), (128, 128)])
+def test_deviations_in_the_mean(d, page):
+    """Relative errors of sigma, root mean square.  Of a sum of m squares one after another each addition
+    is off by 2^-24 / sqrt(3) of what is there by then, together sqrt(m) / 3 of 2^-24 of the whole; the root
+    halves it and adds, as the scale's product does, 2^-24 / sqrt(3).  Two sums of 32 (blocks of 128 x 128): half of
+    1.3 together with 0.8, that is 1.05 of 2^-24 (one of 64: 1.6, measured 2).  Half as much again is
+    left for the squares, whose mean they are not."""
+    gen = torch.Generator(device="cuda").manual_seed(d + page)
+    n, Hkv = 400, 2
+    k = torch.randn(n, Hkv, page, d, generator=gen, device="cuda").mul_(30).to(E4M3)
+    pool = eta.PagePool(k, k.view(n, Hkv, d, page), torch.full((n, Hkv), 0.02, device="cuda"), torch.ones(n, Hkv, device="cuda"))
+    got = eta.build_page_summaries(pool, torch.arange(n, device="cuda").int().view(1, n), ints(n * page)).sigma[0]
+    x = k.double() * pool.k_scale.double()[..., None, None]
+    want = x.std(2, correction=0).permute(1, 2, 0)
+    assert ((got.double() - want) / want).square().mean().sqrt().item() <= 1.5 * 2.0 ** -24
