@@ -25,9 +25,9 @@
 // 32K 40.9 / 41.6, 16 x 3400 of 64 dims in groups of eight 19.2 / 19.8.
 //
 // Bound by HBM once the caches are long: without the gate, the softmax and p.V the same loads take
-// the same time.  512K tokens, 4 kv heads, d = 128, 283.7 MB of a step's union: 48.4 us (5.9 TB/s; a
-// device copy reads and writes 5.16); 8 ragged sequences of up to 32K, dense: 185 MB in 33.4 us;
-// 16 of up to 64K, 232.5 MB of unions in 48.9 us.  Of these 4 to 6 us are the way to the first
+// the same time.  512K tokens, 4 kv heads, d = 128, 283.7 MB of a step's union: 49.2 us (5.8 TB/s; a
+// device copy reads and writes 5.16); 8 ragged sequences of up to 32K, dense: 185 MB in 33.0 us;
+// 16 of up to 64K, 232.5 MB of unions in 49.5 us.  Of these 4 to 6 us are the way to the first
 // load (length, tile counts, union ids, page, keys: each needs the one before) and the merge; short
 // calls are nothing else.  Tried and not faster: values a unit further ahead in a second buffer,
 // eight wavefronts, three per SIMD, the merge by the last workgroup of a group instead of a launch
