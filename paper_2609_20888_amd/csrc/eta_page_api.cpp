@@ -128,8 +128,9 @@ eta_status_t set_decode(int64_t n_blk_cap, Geom* g) {
 // 512 tokens of 64 dims 0.83, 2048 1.35; 128 dims 256 0.95, 1024 1.46); a step, whose share of blocks grows
 // with the heads of a group, up to 2500 of 64 dims and G = 4 (1024 0.95, 4096 1.15; G = 8, 128 dims: 540
 // tokens 28.8 / 23.5 us).  The more groups, the less the rest of the card can take off them: 128 groups
-// 4000 and 1300 tokens dense, from 200 groups on one stays faster up to a million elements of K, a step's
-// up to two (192 groups of 9700 tokens of 128 dims: 48.8 / 55.7).
+// dense 2600 and 1300 tokens (2048 of 64 dims 0.88, 4096 0.99; 1448 of 128 1.09, 2048 1.31), from 200
+// groups on one stays faster up to a million elements of K, a step's up to two (192 groups of 9700 tokens
+// of 128 dims: 48.8 / 55.7 us).
 //
 // Else 256 workgroups in all, one a compute unit of the two that fit at once.  Batches are of different
 // lengths, and 512 even them out: dense from 48 MiB (64 MiB of 16 groups, 256 / 512: equal lengths 1.00 /
